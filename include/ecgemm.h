@@ -324,6 +324,65 @@ ecgemm_status_t ecgemm_product(ecgemm_handle_t handle, int64_t M, int64_t N, int
                                const void *packedA, const void *packedB, float beta, float *C, int64_t ldc,
                                ecgemm_mode_t mode);
 
+/*
+ * Grouped products.  Columns, or the depth, come in `groups` runs of any lengths, which only the GPU knows: `offsets` is a
+ * device array of groups + 1 64-bit integers, not decreasing, group g being offsets[g] .. offsets[g + 1] - 1 (possibly
+ * none).  In a program with row-major tensors a column here is a token, and a group the tokens of one expert or request.
+ * The calls only launch kernels on the handle's stream; they read the offsets on the GPU, so these may be written by kernels
+ * enqueued before, and a captured call replays with the offsets of the day.  Offsets that are negative, beyond the
+ * operand, or decrease leave the results unspecified but nothing outside the operands is touched.
+ *
+ * Both modes of the method (ECGEMM_ERR_UNSUPPORTED for the others and for ECGEMM_MODE_AUTO), and the handle's pre-scaling
+ * (ecgemm_set_scaling).  A forced kernel shape and the timing switch do not matter.  Leading dimensions of the operands up
+ * to 2^21; M, N, K and the number of groups below 2^31.  No workspace is needed, and each call runs on the handle's device
+ * whichever one is current.
+ *
+ * ecgemm_sgemm_grouped, groups of columns (a layer of experts; with transA the other way round its input's gradient):
+ *     C(:, j) <- alpha * op(A_g) * op(B)(:, j) + beta * C(:, j)      for every column j of every group g
+ *   A_g = A + g strideA; op(A_g) is M x K, op(B) is K x N, C is M x N, stored as for ecgemm_sgemm.  Columns in no group (before
+ *   offsets[0], from offsets[groups] on) are left as they are, and so are those of op(B): never read.  strideA may be 0.
+ *
+ * ecgemm_sgemm_grouped_depth, groups of the depth (the gradient of the experts' weights):
+ *     C_g <- alpha * op(A)(:, k's of g) * op(B)(k's of g, :) + beta * C_g
+ *   op(A) is M x K, op(B) is K x N, C_g = C + g strideC is M x N.  A group without any depth gives C_g <- beta * C_g.
+ *
+ * beta == 0: C is not read.  K == 0 or alpha == 0: A and B are not read.  C must not overlap A or B.
+ */
+ecgemm_status_t ecgemm_sgemm_grouped(ecgemm_handle_t handle, ecgemm_op_t transA, ecgemm_op_t transB, int64_t groups,
+                                     int64_t M, int64_t N, int64_t K, float alpha, const float *A, int64_t lda,
+                                     int64_t strideA, const float *B, int64_t ldb, const int64_t *offsets, float beta,
+                                     float *C, int64_t ldc, ecgemm_mode_t mode);
+ecgemm_status_t ecgemm_sgemm_grouped_depth(ecgemm_handle_t handle, ecgemm_op_t transA, ecgemm_op_t transB, int64_t groups,
+                                           int64_t M, int64_t N, int64_t K, float alpha, const float *A, int64_t lda,
+                                           const float *B, int64_t ldb, const int64_t *offsets, float beta, float *C,
+                                           int64_t ldc, int64_t strideC, ecgemm_mode_t mode);
+
+/*
+ * A projection shared by all columns with a low-rank adapter for each group of them:
+ *     H(:, j) <- op(D_a) * op(B)(:, j)                                                       (rank x N)
+ *     C(:, j) <- alpha * op(A) * op(B)(:, j) + scales[a] * op(U_a) * H(:, j) + beta * C(:, j)
+ * for the columns j of group g, a = index[g] (device, one 32-bit integer per group; the same adapter may serve many groups).
+ * A column in no group, or whose group's index is negative or not below `adapters`, has no adapter: C gets the projection
+ * alone and H is zero there.  Groups, offsets, modes and limits as in ecgemm_sgemm_grouped.
+ *   A, B, C, alpha, beta, M, N, K: as in ecgemm_sgemm, all N columns.
+ *   D_a = D + a strideD: op(D_a) is rank x K, ldd >= (transD == N ? rank : K)
+ *   U_a = U + a strideU: op(U_a) is M x rank, ldu >= (transU == N ? M : rank)
+ *   scales: device, one factor per adapter; NULL: 1.
+ *   H: device, FP32, rank x N column-major, ldh >= rank; written for all N columns.  It is an output because the backward
+ *      pass needs it: with G the gradient of C, the gradient of op(B) is this same call on G with op(A)^T in A's place, U^T in
+ *      D's and D^T in U's, which leaves U^T G in its H; the gradients of U and D are ecgemm_sgemm_grouped_depth of G with H,
+ *      and of that call's H with B.
+ * rank at most 1024; adapters below 2^31.  The projection uses the handle's workspace as ecgemm_sgemm does
+ * (ecgemm_workspace_size for M, N, K says how much).  C and H must not overlap each other or anything else.
+ */
+ecgemm_status_t ecgemm_sgemm_adapters(ecgemm_handle_t handle, ecgemm_op_t transA, ecgemm_op_t transB, int64_t M, int64_t N,
+                                      int64_t K, float alpha, const float *A, int64_t lda, const float *B, int64_t ldb,
+                                      int64_t groups, const int64_t *offsets, const int32_t *index, int64_t adapters,
+                                      int64_t rank, ecgemm_op_t transD, const float *D, int64_t ldd, int64_t strideD,
+                                      ecgemm_op_t transU, const float *U, int64_t ldu, int64_t strideU,
+                                      const float *scales, float *H, int64_t ldh, float beta, float *C, int64_t ldc,
+                                      ecgemm_mode_t mode);
+
 /* Bytes ecgemm_split writes for a rows x depth operand.  `bytes` is a host pointer. */
 ecgemm_status_t ecgemm_split_size(int64_t rows, int64_t depth, ecgemm_mode_t mode, size_t *bytes);
 

@@ -24,6 +24,7 @@ SHAPE_AUTO, SHAPE_256x128_W4, SHAPE_128x128_X2, SHAPE_64x64_FUSED, SHAPE_32x32_F
 
 EXPORTS = ["ecgemm_create", "ecgemm_destroy", "ecgemm_set_stream", "ecgemm_workspace_size", "ecgemm_plan_info", "ecgemm_set_workspace",
            "ecgemm_sgemm", "ecgemm_sgemm_scaled", "ecgemm_sgemm_noalloc", "ecgemm_auto_choice", "ecgemm_last_error_argument", "ecgemm_row_scales", "ecgemm_set_shape", "ecgemm_debug_set_tile_order", "ecgemm_debug_tile_order", "ecgemm_debug_one_pass", "ecgemm_set_scaling", "ecgemm_exponent_range", "ecgemm_choose_mode", "ecgemm_product", "ecgemm_split", "ecgemm_split_size", "ecgemm_debug_mfma", "ecgemm_debug_mfma_rate", "ecgemm_set_timing", "ecgemm_get_timing",
+           "ecgemm_sgemm_grouped", "ecgemm_sgemm_grouped_depth", "ecgemm_sgemm_adapters",
            "ecgemm_last_error_string", "ecgemm_status_string"]
 
 
@@ -65,6 +66,12 @@ def _load() -> ctypes.CDLL:
     lib.ecgemm_auto_choice.argtypes = [vp, ctypes.POINTER(ctypes.c_int), ctypes.POINTER(ctypes.c_int)]
     lib.ecgemm_sgemm_scaled.argtypes = [vp, ctypes.c_int, ctypes.c_int, i64, i64, i64, f32, vp, i64, vp, i64, f32, vp, i64,
                                         ctypes.c_int, vp, vp]
+    lib.ecgemm_sgemm_grouped.argtypes = [vp, ctypes.c_int, ctypes.c_int, i64, i64, i64, i64, f32, vp, i64, i64, vp, i64, vp, f32, vp, i64,
+                                         ctypes.c_int]
+    lib.ecgemm_sgemm_grouped_depth.argtypes = [vp, ctypes.c_int, ctypes.c_int, i64, i64, i64, i64, f32, vp, i64, vp, i64, vp, f32, vp, i64, i64,
+                                               ctypes.c_int]
+    lib.ecgemm_sgemm_adapters.argtypes = [vp, ctypes.c_int, ctypes.c_int, i64, i64, i64, f32, vp, i64, vp, i64, i64, vp, vp, i64, i64,
+                                          ctypes.c_int, vp, i64, i64, ctypes.c_int, vp, i64, i64, vp, vp, i64, f32, vp, i64, ctypes.c_int]
     lib.ecgemm_row_scales.argtypes = [vp, ctypes.c_int, i64, i64, vp, i64, ctypes.c_int, vp]
     lib.ecgemm_set_shape.argtypes = [vp, ctypes.c_int]
     lib.ecgemm_debug_set_tile_order.argtypes = [vp, ctypes.c_int, ctypes.c_int, ctypes.c_int]
@@ -185,6 +192,27 @@ class Handle:
                      beta: float, C, ldc: int, mode: int, row_log2_scale_a, col_log2_scale_b):
         self._check(_lib.ecgemm_sgemm_scaled(self._h, transA, transB, M, N, K, alpha, _ptr(A), lda, _ptr(B), ldb, beta,
                                              _ptr(C), ldc, mode, _ptr(row_log2_scale_a), _ptr(col_log2_scale_b)))
+
+    def sgemm_grouped(self, transA: int, transB: int, groups: int, M: int, N: int, K: int, alpha: float, A, lda: int, strideA: int,
+                      B, ldb: int, offsets, beta: float, C, ldc: int, mode: int):
+        """offsets: int64 tensor of groups + 1 entries on the device."""
+        self._check(_lib.ecgemm_sgemm_grouped(self._h, transA, transB, groups, M, N, K, alpha, _ptr(A), lda, strideA, _ptr(B), ldb,
+                                              _ptr(offsets), beta, _ptr(C), ldc, mode))
+
+    def sgemm_grouped_depth(self, transA: int, transB: int, groups: int, M: int, N: int, K: int, alpha: float, A, lda: int, B, ldb: int,
+                            offsets, beta: float, C, ldc: int, strideC: int, mode: int):
+        """offsets: int64 tensor of groups + 1 entries on the device."""
+        self._check(_lib.ecgemm_sgemm_grouped_depth(self._h, transA, transB, groups, M, N, K, alpha, _ptr(A), lda, _ptr(B), ldb,
+                                                    _ptr(offsets), beta, _ptr(C), ldc, strideC, mode))
+
+    def sgemm_adapters(self, transA: int, transB: int, M: int, N: int, K: int, alpha: float, A, lda: int, B, ldb: int, groups: int,
+                       offsets, index, adapters: int, rank: int, transD: int, D, ldd: int, strideD: int, transU: int, U, ldu: int,
+                       strideU: int, scales, H, ldh: int, beta: float, C, ldc: int, mode: int):
+        """offsets: int64 tensor of groups + 1 entries, index: int32 tensor of groups entries, scales: float32 tensor of
+        adapters entries or None, all on the device."""
+        self._check(_lib.ecgemm_sgemm_adapters(self._h, transA, transB, M, N, K, alpha, _ptr(A), lda, _ptr(B), ldb, groups,
+                                               _ptr(offsets), _ptr(index), adapters, rank, transD, _ptr(D), ldd, strideD, transU,
+                                               _ptr(U), ldu, strideU, _ptr(scales), _ptr(H), ldh, beta, _ptr(C), ldc, mode))
 
     def row_scales(self, op: int, rows: int, depth: int, src, ld: int, target_exponent: int, log2_scale):
         self._check(_lib.ecgemm_row_scales(self._h, op, rows, depth, _ptr(src), ld, target_exponent, _ptr(log2_scale)))

@@ -1680,3 +1680,5 @@ ecgemm_status_t ecgemm_product(ecgemm_handle_t handle, int64_t M, int64_t N, int
 }
 
 }  // extern "C"
+
+#include "grouped_calls.hpp"

@@ -1,0 +1,270 @@
+// Host side of the grouped products (see "Grouped products" in include/ecgemm.h): argument checks and launches.  Part of
+// ecgemm.hip, whose context, error and workspace helpers it uses.
+#pragma once
+
+namespace {
+
+// The calls of this file run on the handle's device, whichever is current.
+struct OnDeviceOf {
+  int before = -1;
+  hipError_t error = hipSuccess;
+  explicit OnDeviceOf(ecgemm_handle_t h) {
+    int now = 0;
+    error = hipGetDevice(&now);
+    if (error == hipSuccess && now != h->device) {
+      error = hipSetDevice(h->device);
+      if (error == hipSuccess) before = now;
+    }
+  }
+  ~OnDeviceOf() {
+    if (before >= 0) (void)hipSetDevice(before);
+  }
+};
+
+typedef void (*grouped_fn_t)(GroupedParams);
+template <int METHOD, bool SCALED>
+grouped_fn_t grouped_kernel_of(bool depth_a, bool depth_b) {
+  return depth_a ? (depth_b ? grouped_kernel<METHOD, true, true, SCALED> : grouped_kernel<METHOD, true, false, SCALED>)
+                 : (depth_b ? grouped_kernel<METHOD, false, true, SCALED> : grouped_kernel<METHOD, false, false, SCALED>);
+}
+
+constexpr int64_t kGroupedMostTiles = 1 << 30;
+int64_t tiles_of(int64_t v) { return (v + kGroupedTile - 1) / kGroupedTile; }
+// Most tiles that a call with groups of columns, or all that one with groups of the depth can have in one launch.
+int64_t most_grouped_tiles(bool along_depth, int64_t groups, int64_t M, int64_t N) {
+  const int64_t g = std::min<int64_t>(groups, kGroupsPerLaunch);
+  return along_depth ? g * tiles_of(M) * tiles_of(N) : tiles_of(M) * (N / kGroupedTile + std::min(g, N));
+}
+
+// Everything about the call is checked; gp.groups and what goes with it is filled in here.
+ecgemm_status_t launch_grouped(ecgemm_handle_t h, ecgemm_mode_t mode, bool depth_a, bool depth_b, int64_t groups, GroupedParams gp) {
+  const bool scaled = h->log2_scale_a != 0 || h->log2_scale_b != 0;
+  gp.prescale_a = std::ldexp(1.0f, h->log2_scale_a);
+  gp.prescale_b = std::ldexp(1.0f, h->log2_scale_b);
+  gp.out_scale = std::ldexp(1.0f, -(h->log2_scale_a + h->log2_scale_b));
+  gp.tiles_m = (int)tiles_of(gp.M);
+  gp.tiles_n = gp.along_depth ? (int)tiles_of(gp.N) : 0;
+  const grouped_fn_t kernel = mode == ECGEMM_MODE_FP16_SPLIT
+                                  ? (scaled ? grouped_kernel_of<kMethodFp16Split, true>(depth_a, depth_b) : grouped_kernel_of<kMethodFp16Split, false>(depth_a, depth_b))
+                                  : (scaled ? grouped_kernel_of<kMethodBf16Full, true>(depth_a, depth_b) : grouped_kernel_of<kMethodBf16Full, false>(depth_a, depth_b));
+  const GroupedParams whole = gp;
+  for (int64_t first = 0; first < groups; first += kGroupsPerLaunch) {
+    gp.groups = (int)std::min<int64_t>(groups - first, kGroupsPerLaunch);
+    gp.offsets = whole.offsets + first;
+    if (whole.index) gp.index = whole.index + first;
+    else gp.A = whole.A + first * whole.stride_a;
+    gp.C = whole.C + first * whole.stride_c;
+    const int64_t tiles = most_grouped_tiles(gp.along_depth, gp.groups, gp.M, gp.N);
+    const int64_t grid = std::max(std::min<int64_t>(tiles, h->compute_units), (tiles + kGroupedTilesPerBlock - 1) / kGroupedTilesPerBlock);
+    void* args[] = {&gp};
+    ECGEMM_HIP(h, hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)grid), dim3(kGroupedThreads), args, 0, h->stream));
+  }
+  return ECGEMM_OK;
+}
+
+// Modes the grouped products run in: those of the method.
+ecgemm_status_t check_grouped_mode(ecgemm_handle_t h, int mode, int position, const char* function) {
+  if (!valid_mode_or_auto(mode)) return bad_arg(h, position, (std::string(function) + ": unknown mode").c_str());
+  if (mode != ECGEMM_MODE_FP16_SPLIT && mode != ECGEMM_MODE_BF16_FULL)
+    return fail(h, ECGEMM_ERR_UNSUPPORTED, std::string(function) + ": ECGEMM_MODE_FP16_SPLIT or ECGEMM_MODE_BF16_FULL", position);
+  return ECGEMM_OK;
+}
+#define ECGEMM_ARG(h, bad, position, what) \
+  do {                                     \
+    if (bad) return bad_arg((h), (position), what); \
+  } while (0)
+bool bad_offsets(const int64_t* offsets) { return offsets == nullptr || (uintptr_t)offsets % 8 != 0; }
+
+}  // namespace
+
+extern "C" {
+
+ecgemm_status_t ecgemm_sgemm_grouped(ecgemm_handle_t handle, ecgemm_op_t transA, ecgemm_op_t transB, int64_t groups, int64_t M,
+                                     int64_t N, int64_t K, float alpha, const float* A, int64_t lda, int64_t strideA,
+                                     const float* B, int64_t ldb, const int64_t* offsets, float beta, float* C, int64_t ldc,
+                                     ecgemm_mode_t mode) {
+  ecgemm_handle_t h = handle;
+  if (!h) return ECGEMM_ERR_INVALID_ARG;
+  ECGEMM_ARG(h, !valid_op(transA), 2, "ecgemm_sgemm_grouped: bad transA");
+  ECGEMM_ARG(h, !valid_op(transB), 3, "ecgemm_sgemm_grouped: bad transB");
+  ECGEMM_ARG(h, groups < 0, 4, "ecgemm_sgemm_grouped: negative number of groups");
+  ECGEMM_ARG(h, M < 0, 5, "ecgemm_sgemm_grouped: negative M");
+  ECGEMM_ARG(h, N < 0, 6, "ecgemm_sgemm_grouped: negative N");
+  ECGEMM_ARG(h, K < 0, 7, "ecgemm_sgemm_grouped: negative K");
+  const ecgemm_status_t st = check_grouped_mode(h, (int)mode, 18, "ecgemm_sgemm_grouped");
+  if (st != ECGEMM_OK) return st;
+  if (groups == 0 || M == 0 || N == 0) return ECGEMM_OK;
+  ECGEMM_ARG(h, groups > INT_MAX, 4, "ecgemm_sgemm_grouped: too many groups");
+  ECGEMM_ARG(h, M > INT_MAX, 5, "ecgemm_sgemm_grouped: M too large");
+  ECGEMM_ARG(h, N > INT_MAX, 6, "ecgemm_sgemm_grouped: N too large");
+  ECGEMM_ARG(h, most_grouped_tiles(false, groups, M, N) > kGroupedMostTiles, 5, "ecgemm_sgemm_grouped: M x N too large");
+  ECGEMM_ARG(h, bad_offsets(offsets), 14, "ecgemm_sgemm_grouped: null or misaligned offsets");
+  ECGEMM_ARG(h, !C, 16, "ecgemm_sgemm_grouped: C is null");
+  ECGEMM_ARG(h, ldc < M, 17, "ecgemm_sgemm_grouped: ldc < M");
+  if (alpha == 0.0f) K = 0;  // A and B are not read
+  if (K > 0) {
+    ECGEMM_ARG(h, K > INT_MAX, 7, "ecgemm_sgemm_grouped: K too large");
+    ECGEMM_ARG(h, !A, 9, "ecgemm_sgemm_grouped: A is null");
+    ECGEMM_ARG(h, lda < (transA == ECGEMM_OP_N ? M : K), 10, "ecgemm_sgemm_grouped: lda too small");
+    ECGEMM_ARG(h, lda > kGroupedLargestLd, 10, "ecgemm_sgemm_grouped: lda beyond 2^21");
+    ECGEMM_ARG(h, strideA < 0, 11, "ecgemm_sgemm_grouped: negative strideA");
+    ECGEMM_ARG(h, !B, 12, "ecgemm_sgemm_grouped: B is null");
+    ECGEMM_ARG(h, ldb < (transB == ECGEMM_OP_N ? K : N), 13, "ecgemm_sgemm_grouped: ldb too small");
+    ECGEMM_ARG(h, ldb > kGroupedLargestLd, 13, "ecgemm_sgemm_grouped: ldb beyond 2^21");
+  }
+  const OnDeviceOf device(h);
+  if (device.error != hipSuccess) return hip_fail(h, device.error, "hipSetDevice");
+  GroupedParams gp{};
+  gp.A = A, gp.lda = lda, gp.stride_a = strideA;
+  gp.B = B, gp.ldb = ldb;
+  gp.C = C, gp.ldc = ldc;
+  gp.M = M, gp.N = N, gp.K = K;
+  gp.offsets = offsets;
+  gp.alpha = alpha, gp.beta = beta;
+  return launch_grouped(h, mode, transA == ECGEMM_OP_T, transB == ECGEMM_OP_N, groups, gp);
+}
+
+ecgemm_status_t ecgemm_sgemm_grouped_depth(ecgemm_handle_t handle, ecgemm_op_t transA, ecgemm_op_t transB, int64_t groups,
+                                           int64_t M, int64_t N, int64_t K, float alpha, const float* A, int64_t lda,
+                                           const float* B, int64_t ldb, const int64_t* offsets, float beta, float* C,
+                                           int64_t ldc, int64_t strideC, ecgemm_mode_t mode) {
+  ecgemm_handle_t h = handle;
+  if (!h) return ECGEMM_ERR_INVALID_ARG;
+  ECGEMM_ARG(h, !valid_op(transA), 2, "ecgemm_sgemm_grouped_depth: bad transA");
+  ECGEMM_ARG(h, !valid_op(transB), 3, "ecgemm_sgemm_grouped_depth: bad transB");
+  ECGEMM_ARG(h, groups < 0, 4, "ecgemm_sgemm_grouped_depth: negative number of groups");
+  ECGEMM_ARG(h, M < 0, 5, "ecgemm_sgemm_grouped_depth: negative M");
+  ECGEMM_ARG(h, N < 0, 6, "ecgemm_sgemm_grouped_depth: negative N");
+  ECGEMM_ARG(h, K < 0, 7, "ecgemm_sgemm_grouped_depth: negative K");
+  const ecgemm_status_t st = check_grouped_mode(h, (int)mode, 18, "ecgemm_sgemm_grouped_depth");
+  if (st != ECGEMM_OK) return st;
+  if (groups == 0 || M == 0 || N == 0) return ECGEMM_OK;
+  ECGEMM_ARG(h, groups > INT_MAX, 4, "ecgemm_sgemm_grouped_depth: too many groups");
+  ECGEMM_ARG(h, M > INT_MAX, 5, "ecgemm_sgemm_grouped_depth: M too large");
+  ECGEMM_ARG(h, N > INT_MAX, 6, "ecgemm_sgemm_grouped_depth: N too large");
+  // (each factor is below 2^25, so their product of at most 2^10 2^24 2^24 fits)
+  ECGEMM_ARG(h, most_grouped_tiles(true, groups, M, N) > kGroupedMostTiles, 5, "ecgemm_sgemm_grouped_depth: groups x M x N too large");
+  ECGEMM_ARG(h, bad_offsets(offsets), 13, "ecgemm_sgemm_grouped_depth: null or misaligned offsets");
+  ECGEMM_ARG(h, !C, 15, "ecgemm_sgemm_grouped_depth: C is null");
+  ECGEMM_ARG(h, ldc < M, 16, "ecgemm_sgemm_grouped_depth: ldc < M");
+  ECGEMM_ARG(h, groups > 1 && strideC < (__int128)ldc * (N - 1) + M, 17, "ecgemm_sgemm_grouped_depth: the groups' C overlap");
+  if (alpha == 0.0f) K = 0;
+  if (K > 0) {
+    ECGEMM_ARG(h, K > INT_MAX, 7, "ecgemm_sgemm_grouped_depth: K too large");
+    ECGEMM_ARG(h, !A, 9, "ecgemm_sgemm_grouped_depth: A is null");
+    ECGEMM_ARG(h, lda < (transA == ECGEMM_OP_N ? M : K), 10, "ecgemm_sgemm_grouped_depth: lda too small");
+    ECGEMM_ARG(h, lda > kGroupedLargestLd, 10, "ecgemm_sgemm_grouped_depth: lda beyond 2^21");
+    ECGEMM_ARG(h, !B, 11, "ecgemm_sgemm_grouped_depth: B is null");
+    ECGEMM_ARG(h, ldb < (transB == ECGEMM_OP_N ? K : N), 12, "ecgemm_sgemm_grouped_depth: ldb too small");
+    ECGEMM_ARG(h, ldb > kGroupedLargestLd, 12, "ecgemm_sgemm_grouped_depth: ldb beyond 2^21");
+  }
+  const OnDeviceOf device(h);
+  if (device.error != hipSuccess) return hip_fail(h, device.error, "hipSetDevice");
+  GroupedParams gp{};
+  gp.A = A, gp.lda = lda;
+  gp.B = B, gp.ldb = ldb;
+  gp.C = C, gp.ldc = ldc, gp.stride_c = strideC;
+  gp.M = M, gp.N = N, gp.K = K;
+  gp.offsets = offsets;
+  gp.along_depth = 1;
+  gp.alpha = alpha, gp.beta = beta;
+  return launch_grouped(h, mode, transA == ECGEMM_OP_T, transB == ECGEMM_OP_N, groups, gp);
+}
+
+ecgemm_status_t ecgemm_sgemm_adapters(ecgemm_handle_t handle, ecgemm_op_t transA, ecgemm_op_t transB, int64_t M, int64_t N,
+                                      int64_t K, float alpha, const float* A, int64_t lda, const float* B, int64_t ldb,
+                                      int64_t groups, const int64_t* offsets, const int32_t* index, int64_t adapters,
+                                      int64_t rank, ecgemm_op_t transD, const float* D, int64_t ldd, int64_t strideD,
+                                      ecgemm_op_t transU, const float* U, int64_t ldu, int64_t strideU, const float* scales,
+                                      float* H, int64_t ldh, float beta, float* C, int64_t ldc, ecgemm_mode_t mode) {
+  ecgemm_handle_t h = handle;
+  if (!h) return ECGEMM_ERR_INVALID_ARG;
+  ECGEMM_ARG(h, !valid_op(transA), 2, "ecgemm_sgemm_adapters: bad transA");
+  ECGEMM_ARG(h, !valid_op(transB), 3, "ecgemm_sgemm_adapters: bad transB");
+  ECGEMM_ARG(h, M < 0, 4, "ecgemm_sgemm_adapters: negative M");
+  ECGEMM_ARG(h, N < 0, 5, "ecgemm_sgemm_adapters: negative N");
+  ECGEMM_ARG(h, K < 0, 6, "ecgemm_sgemm_adapters: negative K");
+  ECGEMM_ARG(h, groups < 0, 12, "ecgemm_sgemm_adapters: negative number of groups");
+  ECGEMM_ARG(h, adapters < 0, 15, "ecgemm_sgemm_adapters: negative number of adapters");
+  ECGEMM_ARG(h, rank < 0, 16, "ecgemm_sgemm_adapters: negative rank");
+  ECGEMM_ARG(h, !valid_op(transD), 17, "ecgemm_sgemm_adapters: bad transD");
+  ECGEMM_ARG(h, !valid_op(transU), 21, "ecgemm_sgemm_adapters: bad transU");
+  ecgemm_status_t st = check_grouped_mode(h, (int)mode, 31, "ecgemm_sgemm_adapters");
+  if (st != ECGEMM_OK) return st;
+  if (N == 0) return ECGEMM_OK;
+  ECGEMM_ARG(h, M > INT_MAX, 4, "ecgemm_sgemm_adapters: M too large");
+  ECGEMM_ARG(h, N > INT_MAX, 5, "ecgemm_sgemm_adapters: N too large");
+  ECGEMM_ARG(h, K > INT_MAX, 6, "ecgemm_sgemm_adapters: K too large");
+  ECGEMM_ARG(h, groups > INT_MAX, 12, "ecgemm_sgemm_adapters: too many groups");
+  ECGEMM_ARG(h, adapters > INT_MAX, 15, "ecgemm_sgemm_adapters: too many adapters");
+  ECGEMM_ARG(h, rank > kLargestRank, 16, "ecgemm_sgemm_adapters: rank too large");
+  ECGEMM_ARG(h, most_grouped_tiles(false, groups, M, N) > kGroupedMostTiles, 4, "ecgemm_sgemm_adapters: M x N too large");
+  const bool any = groups > 0 && adapters > 0 && rank > 0;
+  ECGEMM_ARG(h, any && bad_offsets(offsets), 13, "ecgemm_sgemm_adapters: null or misaligned offsets");
+  ECGEMM_ARG(h, any && (!index || (uintptr_t)index % 4 != 0), 14, "ecgemm_sgemm_adapters: null or misaligned index");
+  if (K > 0 && (any || alpha != 0.0f)) {
+    ECGEMM_ARG(h, !B, 10, "ecgemm_sgemm_adapters: B is null");
+    ECGEMM_ARG(h, ldb < (transB == ECGEMM_OP_N ? K : N), 11, "ecgemm_sgemm_adapters: ldb too small");
+    ECGEMM_ARG(h, any && ldb > kGroupedLargestLd, 11, "ecgemm_sgemm_adapters: ldb beyond 2^21");
+  }
+  if (M > 0 && K > 0 && alpha != 0.0f) {
+    ECGEMM_ARG(h, !A, 8, "ecgemm_sgemm_adapters: A is null");
+    ECGEMM_ARG(h, lda < (transA == ECGEMM_OP_N ? M : K), 9, "ecgemm_sgemm_adapters: lda too small");
+  }
+  if (any && K > 0) {
+    ECGEMM_ARG(h, !D, 18, "ecgemm_sgemm_adapters: D is null");
+    ECGEMM_ARG(h, ldd < (transD == ECGEMM_OP_N ? rank : K), 19, "ecgemm_sgemm_adapters: ldd too small");
+    ECGEMM_ARG(h, ldd > kGroupedLargestLd, 19, "ecgemm_sgemm_adapters: ldd beyond 2^21");
+    ECGEMM_ARG(h, strideD < 0, 20, "ecgemm_sgemm_adapters: negative strideD");
+  }
+  if (any && M > 0) {
+    ECGEMM_ARG(h, !U, 22, "ecgemm_sgemm_adapters: U is null");
+    ECGEMM_ARG(h, ldu < (transU == ECGEMM_OP_N ? M : rank), 23, "ecgemm_sgemm_adapters: ldu too small");
+    ECGEMM_ARG(h, ldu > kGroupedLargestLd, 23, "ecgemm_sgemm_adapters: ldu beyond 2^21");
+    ECGEMM_ARG(h, strideU < 0, 24, "ecgemm_sgemm_adapters: negative strideU");
+  }
+  if (rank > 0) {
+    ECGEMM_ARG(h, !H, 26, "ecgemm_sgemm_adapters: H is null");
+    ECGEMM_ARG(h, ldh < rank, 27, "ecgemm_sgemm_adapters: ldh < rank");
+    ECGEMM_ARG(h, ldh > kGroupedLargestLd, 27, "ecgemm_sgemm_adapters: ldh beyond 2^21");
+  }
+  if (M > 0) {
+    ECGEMM_ARG(h, !C, 29, "ecgemm_sgemm_adapters: C is null");
+    ECGEMM_ARG(h, ldc < M, 30, "ecgemm_sgemm_adapters: ldc < M");
+  }
+  const OnDeviceOf device(h);
+  if (device.error != hipSuccess) return hip_fail(h, device.error, "hipSetDevice");
+  // the shared projection
+  if (M > 0) {
+    st = sgemm_common(h, transA, transB, M, N, K, alpha, A, lda, B, ldb, beta, C, ldc, mode, nullptr, nullptr, kWorkspaceOfHandle);
+    if (st != ECGEMM_OK) return st;
+  }
+  if (rank == 0) return ECGEMM_OK;
+  // H = op(D) op(B), zero in every column without an adapter
+  const dim3 grid((unsigned)((rank + 255) / 256), (unsigned)std::min<int64_t>(N, 65535));
+  hipLaunchKernelGGL(scale_c_kernel, grid, dim3(256), 0, h->stream, rank, N, 0.0f, H, ldh);
+  ECGEMM_HIP(h, hipGetLastError());
+  if (!any) return ECGEMM_OK;
+  GroupedParams down{};
+  down.A = D, down.lda = ldd, down.stride_a = strideD;
+  down.B = B, down.ldb = ldb;
+  down.C = H, down.ldc = ldh;
+  down.M = rank, down.N = N, down.K = K;
+  down.offsets = offsets;
+  down.index = index, down.matrices = (int)adapters;
+  down.alpha = 1.0f, down.beta = 0.0f;
+  st = launch_grouped(h, mode, transD == ECGEMM_OP_T, transB == ECGEMM_OP_N, groups, down);
+  if (st != ECGEMM_OK || M == 0) return st;
+  // C += scale op(U) H
+  GroupedParams up{};
+  up.A = U, up.lda = ldu, up.stride_a = strideU;
+  up.B = H, up.ldb = ldh;
+  up.C = C, up.ldc = ldc;
+  up.M = M, up.N = N, up.K = rank;
+  up.offsets = offsets;
+  up.index = index, up.matrices = (int)adapters, up.scales = scales;
+  up.alpha = 1.0f, up.beta = 1.0f;
+  return launch_grouped(h, mode, transU == ECGEMM_OP_T, true, groups, up);
+}
+
+}  // extern "C"

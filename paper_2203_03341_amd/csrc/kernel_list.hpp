@@ -6,6 +6,7 @@
 // them side by side.
 #pragma once
 #include "fused_kernel.hpp"
+#include "grouped_kernel.hpp"
 #include "product_kernel.hpp"
 #include "split_kernels.hpp"
 #include "wide_kernel.hpp"
@@ -68,6 +69,16 @@ typedef ProductConfig<kMethodFp32, 256, 128, 128, 64, 2, 3, 1> Fp32Config;
 #else
 #define ECGEMM_WIDE_GROUP extern
 #endif
+#ifdef ECGEMM_INSTANTIATE_GROUPED_FP16
+#define ECGEMM_GROUPED_FP16_GROUP
+#else
+#define ECGEMM_GROUPED_FP16_GROUP extern
+#endif
+#ifdef ECGEMM_INSTANTIATE_GROUPED_BF16
+#define ECGEMM_GROUPED_BF16_GROUP
+#else
+#define ECGEMM_GROUPED_BF16_GROUP extern
+#endif
 #ifdef ECGEMM_INSTANTIATE_SPLIT
 #define ECGEMM_SPLIT_GROUP
 #else
@@ -123,6 +134,16 @@ ECGEMM_WIDE_GROUP template __global__ void wide_kernel<kMethodFp16Split, false, 
 ECGEMM_WIDE_GROUP template __global__ void wide_kernel<kMethodFp16Split, false, true>(const WideParams);
 ECGEMM_WIDE_GROUP template __global__ void wide_kernel<kMethodFp16Split, true, false>(const WideParams);
 ECGEMM_WIDE_GROUP template __global__ void wide_kernel<kMethodFp16Split, true, true>(const WideParams);
+
+#define ECGEMM_GROUPED_KERNELS_OF(GROUP, METHOD, SCALED)                                                  \
+  GROUP template __global__ void grouped_kernel<METHOD, false, false, SCALED>(const GroupedParams);  \
+  GROUP template __global__ void grouped_kernel<METHOD, false, true, SCALED>(const GroupedParams);   \
+  GROUP template __global__ void grouped_kernel<METHOD, true, false, SCALED>(const GroupedParams);   \
+  GROUP template __global__ void grouped_kernel<METHOD, true, true, SCALED>(const GroupedParams);
+ECGEMM_GROUPED_KERNELS_OF(ECGEMM_GROUPED_FP16_GROUP, kMethodFp16Split, false)
+ECGEMM_GROUPED_KERNELS_OF(ECGEMM_GROUPED_FP16_GROUP, kMethodFp16Split, true)  // for handles with a pre-scaling
+ECGEMM_GROUPED_KERNELS_OF(ECGEMM_GROUPED_BF16_GROUP, kMethodBf16Full, false)
+ECGEMM_GROUPED_KERNELS_OF(ECGEMM_GROUPED_BF16_GROUP, kMethodBf16Full, true)
 
 #define ECGEMM_SPLIT_KERNELS_OF(KIND)                                                                     \
   ECGEMM_SPLIT_GROUP template __global__ void split_kernel<KIND, kSplitKContiguous, false>(const SplitJob);      \

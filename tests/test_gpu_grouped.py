@@ -1,0 +1,612 @@
+"""The grouped products (ecgemm_sgemm_grouped, ecgemm_sgemm_grouped_depth, ecgemm_sgemm_adapters) against the same sums in
+64 bits, at the sizes and contents where they can go wrong.
+
+How far an element may be off, derived: with S = sum over k of |a_k| |b_k| for that element,
+  * FP16 mode: a pair misses its value by 2^-23 of it, both operands 2^-22 together; the product left out is at most
+    2^-11 2^-11 = 2^-22: 2^-21 S.  The residual is a multiple of 2^-24 at the finest, and 2^11 times what it stands for: however
+    small a value, the pair may miss it by half of 2^-24 2^-11, 2^-36, which meets the other operand's value: 2^-36 times the
+    sum of |a_k| and of |b_k| (and that power of two less for an operand that is scaled before the split).  BF16 mode: three
+    terms hold 24 bits, the products left out are below 3 2^-24: less than 2^-21 S again.
+  * the matrix unit adds 16 products to an accumulator at a time and drops what lies below 2^-25 of the largest addend, and
+    rounds: at most (16 2^-25 + 2^-24) S for each 16 of the depth and each of the two accumulators, which do not both reach S:
+    2^-11 S is the other one's, counted as one step more.
+  * the merge, alpha, beta and the last rounding: 4 2^-24 (S |alpha| + |beta| |C|).
+All operands lie in a field of NaN (leading dimensions, what is before and behind them), so that a value read from outside
+would show in the result; all results in a field of one value, so that a value written outside would."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+MODES = ["fp16", "bf16"]
+
+
+def _ec():
+    import paper_2203_03341_amd as ec
+    return ec
+
+
+def _mode(mode):
+    ec = _ec()
+    return ec.MODE_FP16_SPLIT if mode == "fp16" else ec.MODE_BF16_FULL
+
+
+@pytest.fixture(scope="module")
+def handle():
+    import torch
+    h = _ec().Handle()
+    h.set_stream(torch.cuda.current_stream().cuda_stream)
+    yield h
+    torch.cuda.synchronize()
+    h.destroy()
+
+
+class Field:
+    """`count` column-major rows x cols matrices with leading dimension ld, in a field of `fill`"""
+
+    def __init__(self, rows, cols, pad=0, count=1, gap=0, fill=float("nan"), values=None, wide=False, gen=None, scale=1.0, offset=5):
+        import torch
+        self.rows, self.cols, self.ld, self.count = rows, cols, max(1, rows + pad), count
+        self.stride = self.ld * max(cols, 1) + gap
+        self.fill, self.at = fill, 64 + offset
+        self.store = torch.full((self.at + self.stride * count + 64,), fill, dtype=torch.float32, device="cuda")
+        if values is None and gen is not None:
+            values = torch.randn((count, cols, rows), generator=gen, device="cuda", dtype=torch.float64) * scale
+            if wide:
+                values *= torch.exp2(torch.randint(-40, 21, (count, cols, 1), generator=gen, device="cuda").double())
+            values = values.float()
+        if values is not None:
+            self.view().copy_(values)
+
+    def view(self):
+        """(count, cols, rows): [g, j, i] is element (i, j) of matrix g"""
+        return self.store.as_strided((self.count, self.cols, self.rows), (self.stride, self.ld, 1), self.at)
+
+    def ptr(self):
+        return self.store.data_ptr() + 4 * self.at
+
+    def matrix(self, trans, g=0):
+        """op of matrix g in 64 bits, (rows of op, columns of op)"""
+        v = self.view()[g].double()
+        return v if trans == "T" else v.t()
+
+
+def _offsets(sizes, start=0):
+    import torch
+    return torch.tensor(np.concatenate([[start], start + np.cumsum(sizes)]), dtype=torch.int64, device="cuda")
+
+
+def _allowed(a, b, mode, alpha, beta, before, scaling=(0, 0)):
+    """a: M x depth, b: depth x N, in 64 bits"""
+    import math
+    S, depth = a.abs() @ b.abs(), a.shape[1]
+    if mode == "fp16":
+        S = S + 2.0 ** 21 * (2.0 ** (-36 - scaling[0]) * b.abs().sum(0)[None, :] + 2.0 ** (-36 - scaling[1]) * a.abs().sum(1)[:, None])
+    step = 16 * 2.0 ** -25 + 2.0 ** -24
+    bound = (2.0 ** -21 + (math.ceil(depth / 16) + 1) * step) * abs(alpha) * S + 4 * 2.0 ** -24 * abs(alpha) * S
+    return bound + (4 * 2.0 ** -24 * abs(beta) * before.abs() if beta else 0.0) + 1e-37
+
+
+def _ops(trans):
+    ec = _ec()
+    return {"N": ec.OP_N, "T": ec.OP_T}[trans]
+
+
+def _gen(seed):
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def _run_columns(handle, trans, mode, M, K, sizes, start=0, behind=0, alpha=1.0, beta=0.0, pad=(0, 0, 0), wide=False, seed=1, offset=5,
+                 shared=False, scaling=(0, 0)):
+    """One call, checked element by element; returns C's field."""
+    import torch
+    ec, gen = _ec(), _gen(seed)
+    N = start + sum(sizes) + behind
+    groups = len(sizes)
+    a_shape = (M, K) if trans[0] == "N" else (K, M)
+    b_shape = (K, N) if trans[1] == "N" else (N, K)
+    A = Field(*a_shape, pad=pad[0], count=1 if shared else groups, gap=pad[0], gen=gen, scale=0.5, offset=offset)
+    B = Field(*b_shape, pad=pad[1], gen=gen, wide=wide and trans[1] == "N", offset=offset)
+    C = Field(M, N, pad=pad[2], fill=7.0, offset=offset)
+    if beta:
+        C.view().copy_(torch.randn((1, N, M), generator=gen, device="cuda"))
+    # what no group holds is never read
+    outside = [*range(start), *range(start + sum(sizes), N)]
+    b_cols = B.view()[0] if trans[1] == "N" else B.view()[0].t()
+    if outside:
+        b_cols[outside] = float("nan")
+    before = C.store.clone()
+    offs = _offsets(sizes, start)
+    handle.sgemm_grouped(_ops(trans[0]), _ops(trans[1]), groups, M, N, K, alpha, A.ptr(), A.ld, 0 if shared else A.stride, B.ptr(), B.ld, offs,
+                         beta, C.ptr(), C.ld, _mode(mode))
+    torch.cuda.synchronize()
+    want = before.clone()
+    expected = want.as_strided((N, M), (C.ld, 1), C.at)
+    got = C.view()[0]
+    at = start
+    for g, n in enumerate(sizes):
+        if n:
+            a, b = A.matrix(trans[0], 0 if shared else g), B.matrix(trans[1])[:, at:at + n]
+            c_in = expected[at:at + n].t().double()
+            exact = alpha * (a @ b) + (beta * c_in if beta else 0.0)
+            allowed = _allowed(a, b, mode, alpha, beta, c_in, scaling)
+            off = (got[at:at + n].t().double() - exact).abs()
+            assert bool((off <= allowed).all()), (trans, mode, M, K, g, n, float((off / allowed).max()))
+            expected[at:at + n] = got[at:at + n]
+        at += n
+    assert torch.equal(C.store, want)       # nothing else was written
+    return C
+
+
+@pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("trans", ["TN", "NN", "TT", "NT"])
+def test_columns_in_every_storage_order(handle, trans, mode):
+    _run_columns(handle, trans, mode, 200, 96, [37, 0, 1, 128, 129, 0, 260], start=3, behind=11, pad=(3, 1, 5))
+    _run_columns(handle, trans, mode, 384, 512, [256, 128, 384], alpha=1.5, beta=-0.5)
+
+
+@pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("K", [1, 2, 3, 4, 5, 31, 32, 33, 63, 64, 65, 127, 129, 192, 257, 515])
+def test_columns_at_every_kind_of_depth(handle, mode, K):
+    for trans in ("TN", "NT"):
+        _run_columns(handle, trans, mode, 130, K, [5, 150, 64], behind=2, seed=K, pad=(1, 2, 0))
+
+
+@pytest.mark.parametrize("M", [1, 2, 3, 4, 5, 63, 64, 127, 128, 131, 258])
+def test_columns_with_few_rows_and_odd_ones(handle, M):
+    for trans in ("TN", "NN", "TT"):
+        for mode in MODES:
+            _run_columns(handle, trans, mode, M, 70, [1, 2, 3, 129], seed=M)
+
+
+@pytest.mark.parametrize("sizes", [[0], [1], [0, 0, 0], [1] * 40, [0, 0, 300, 0], [513, 1, 0, 2], [128] * 9])
+def test_columns_in_groups_of_every_size(handle, sizes):
+    for mode in MODES:
+        _run_columns(handle, "TN", mode, 140, 130, sizes, start=1, behind=1)
+    _run_columns(handle, "NT", "fp16", 140, 130, sizes, start=1, behind=1)
+
+
+def test_columns_of_any_magnitude_in_bf16_mode(handle):
+    _run_columns(handle, "TN", "bf16", 150, 300, [40, 200], wide=True)
+
+
+def test_columns_many_groups_and_tiles(handle):
+    rng = np.random.RandomState(3)
+    _run_columns(handle, "TN", "fp16", 40, 33, list(rng.randint(0, 4, 2500)))         # several launches
+    _run_columns(handle, "TN", "fp16", 700, 150, list(rng.randint(0, 900, 30)))       # several tiles for every block
+    _run_columns(handle, "NN", "bf16", 640, 150, list(rng.randint(0, 900, 30)), beta=1.0)
+
+
+def test_columns_shared_matrix_and_scaling(handle):
+    _run_columns(handle, "TN", "fp16", 130, 100, [60, 70], shared=True)
+    handle.set_scaling(6, -3)
+    try:
+        for mode in MODES:
+            _run_columns(handle, "TN", mode, 130, 100, [60, 70], alpha=0.5, beta=2.0, scaling=(6, -3))
+            _run_columns(handle, "NT", mode, 130, 300, [60, 70], scaling=(6, -3))
+            _run_depth(handle, "NT", mode, 130, 70, [5, 300], scaling=(6, -3))
+    finally:
+        handle.set_scaling(0, 0)
+
+
+def _run_depth(handle, trans, mode, M, N, sizes, start=0, behind=0, alpha=1.0, beta=0.0, pad=(0, 0, 0), wide=False, seed=1, offset=5,
+               scaling=(0, 0)):
+    import torch
+    gen = _gen(seed)
+    K = start + sum(sizes) + behind
+    groups = len(sizes)
+    a_shape = (M, K) if trans[0] == "N" else (K, M)
+    b_shape = (K, N) if trans[1] == "N" else (N, K)
+    A = Field(*a_shape, pad=pad[0], gen=gen, wide=wide and trans[0] == "N", offset=offset)
+    B = Field(*b_shape, pad=pad[1], gen=gen, offset=offset)
+    outside = [*range(start), *range(start + sum(sizes), K)]
+    if outside:
+        (A.view()[0] if trans[0] == "N" else A.view()[0].t())[outside] = float("nan")
+        (B.view()[0] if trans[1] == "T" else B.view()[0].t())[outside] = float("nan")
+    C = Field(M, N, pad=pad[2], count=groups, gap=pad[2], fill=7.0, offset=offset)
+    if beta:
+        C.view().copy_(torch.randn((groups, N, M), generator=gen, device="cuda"))
+    before = C.store.clone()
+    handle.sgemm_grouped_depth(_ops(trans[0]), _ops(trans[1]), groups, M, N, K, alpha, A.ptr(), A.ld, B.ptr(), B.ld, _offsets(sizes, start),
+                               beta, C.ptr(), C.ld, C.stride, _mode(mode))
+    torch.cuda.synchronize()
+    want = before.clone()
+    expected = want.as_strided((groups, N, M), (C.stride, C.ld, 1), C.at)
+    at = start
+    for g, n in enumerate(sizes):
+        c_in = expected[g].t().double()
+        a, b = A.matrix(trans[0])[:, at:at + n], B.matrix(trans[1])[at:at + n]
+        exact = alpha * (a @ b) + (beta * c_in if beta else 0.0)
+        off = (C.view()[g].t().double() - exact).abs()
+        allowed = _allowed(a, b, mode, alpha, beta, c_in, scaling)
+        assert bool((off <= allowed).all()), (trans, mode, M, N, g, n, float((off / allowed).max()))
+        expected[g] = C.view()[g]
+        at += n
+    assert torch.equal(C.store, want)
+    return C
+
+
+@pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("trans", ["NT", "NN", "TT", "TN"])
+def test_depth_in_every_storage_order(handle, trans, mode):
+    _run_depth(handle, trans, mode, 200, 130, [37, 0, 1, 2, 3, 4, 5, 64, 65, 300], start=3, behind=11, pad=(3, 1, 5))
+    _run_depth(handle, trans, mode, 384, 256, [128, 512, 0], alpha=1.5, beta=-0.5)
+
+
+@pytest.mark.parametrize("M,N", [(1, 1), (3, 5), (127, 129), (2, 260), (260, 2), (128, 128)])
+def test_depth_with_few_rows_and_columns(handle, M, N):
+    for trans in ("NT", "TN", "TT"):
+        for mode in MODES:
+            _run_depth(handle, trans, mode, M, N, [1, 33, 0, 200], behind=1, seed=M)
+
+
+def test_depth_many_groups_and_tiles(handle):
+    rng = np.random.RandomState(4)
+    _run_depth(handle, "NT", "fp16", 20, 30, list(rng.randint(0, 4, 2100)))
+    _run_depth(handle, "NT", "bf16", 300, 400, list(rng.randint(0, 200, 60)), beta=1.0, wide=True)
+
+
+def _run_adapters(handle, mode, M, N, K, rank, sizes, index, adapters, trans="TNTT", start=0, alpha=1.0, beta=0.0, scales=True, pad=0,
+                  wide=False, seed=1):
+    """trans: of A, B, D, U"""
+    import torch
+    gen = _gen(seed)
+
+    def operand(rows, cols, t, **more):
+        return Field(rows, cols, gen=gen, pad=pad, **more) if t == "N" else Field(cols, rows, gen=gen, pad=pad, **more)
+
+    A = operand(M, K, trans[0], scale=K ** -0.5 if K else 1.0)
+    B = operand(K, N, trans[1], wide=wide and trans[1] == "N")
+    D = operand(rank, K, trans[2], count=max(adapters, 1), gap=pad, scale=K ** -0.5 if K else 1.0)
+    U = operand(M, rank, trans[3], count=max(adapters, 1), gap=pad, scale=max(rank, 1) ** -0.5)
+    s = 0.5 + torch.rand(max(adapters, 1), generator=gen, device="cuda")
+    H, C = Field(rank, N, pad=pad, fill=7.0), Field(M, N, pad=pad, fill=7.0)
+    if beta:
+        C.view().copy_(torch.randn((1, N, M), generator=gen, device="cuda"))
+    before_c, before_h = C.store.clone(), H.store.clone()
+    handle.sgemm_adapters(_ops(trans[0]), _ops(trans[1]), M, N, K, alpha, A.ptr(), A.ld, B.ptr(), B.ld, len(sizes), _offsets(sizes, start),
+                          torch.tensor(index, dtype=torch.int32, device="cuda"), adapters, rank, _ops(trans[2]), D.ptr(), D.ld, D.stride,
+                          _ops(trans[3]), U.ptr(), U.ld, U.stride, s if scales else None, H.ptr(), H.ld, beta, C.ptr(), C.ld, _mode(mode))
+    torch.cuda.synchronize()
+    a, b = A.matrix(trans[0]), B.matrix(trans[1])
+    c_in = before_c.as_strided((N, M), (C.ld, 1), C.at).t().double()
+    exact = alpha * (a @ b) + (beta * c_in if beta else 0.0)
+    allowed = _allowed(a, b, mode, alpha, beta, c_in)
+    hidden = torch.zeros((rank, N), dtype=torch.float64, device="cuda")
+    hidden_allowed = torch.full((rank, N), 1e-37, dtype=torch.float64, device="cuda")
+    at = start
+    for g, n in enumerate(sizes):
+        if n and 0 <= index[g] < adapters and rank:
+            d, u = D.matrix(trans[2], index[g]), U.matrix(trans[3], index[g])
+            x, factor = b[:, at:at + n], float(s[index[g]]) if scales else 1.0
+            hidden[:, at:at + n] = d @ x
+            hidden_allowed[:, at:at + n] = _allowed(d, x, mode, 1.0, 0.0, None)
+            # (what H is off by goes through U; the sum meets C in one more rounding)
+            h = hidden[:, at:at + n]
+            exact[:, at:at + n] += factor * (u @ h)
+            allowed[:, at:at + n] += (factor * (u.abs() @ hidden_allowed[:, at:at + n]) + _allowed(u, h, mode, factor, 0.0, None)
+                                      + 2.0 ** -23 * exact[:, at:at + n].abs())
+        at += n
+    off = (H.view()[0].t().double() - hidden).abs()
+    assert bool((off <= hidden_allowed).all()), ("H", mode, M, N, K, rank, float((off / hidden_allowed).max()))
+    off = (C.view()[0].t().double() - exact).abs()
+    assert bool((off <= allowed).all()), ("C", mode, M, N, K, rank, float((off / allowed).max()))
+    for field, before in ((C, before_c), (H, before_h)):
+        field.view().copy_(before.as_strided(field.view().shape, field.view().stride(), field.at))
+        assert torch.equal(field.store, before)     # nothing else was written
+
+
+@pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("trans", ["TNTT", "NNNN", "TTTN", "NTNT"])
+def test_adapters_in_every_storage_order(handle, trans, mode):
+    _run_adapters(handle, mode, 200, 190, 150, 12, [30, 1, 0, 100, 40], [1, -1, 0, 2, 1], 3, trans=trans, start=5, pad=3)
+    _run_adapters(handle, mode, 256, 256, 128, 16, [128, 128], [0, 1], 2, trans=trans, alpha=1.5, beta=0.5)
+
+
+@pytest.mark.parametrize("rank", [1, 2, 3, 4, 7, 8, 16, 20, 33, 64, 65, 130])
+def test_adapters_of_every_rank(handle, rank):
+    for mode in MODES:
+        _run_adapters(handle, mode, 140, 75, 260, rank, [1, 1, 2, 40, 9], [3, 0, 1, 2, -1], 4, seed=rank)
+
+
+@pytest.mark.parametrize("N", [1, 2, 5, 16, 17, 31, 32, 33, 64, 65])
+def test_adapters_of_single_tokens(handle, N):
+    """A decoding step: a token and an adapter per request."""
+    rng = np.random.RandomState(N)
+    for mode in MODES:
+        _run_adapters(handle, mode, 300, N, 500, 16, [1] * N, list(rng.randint(-1, 6, N)), 6, seed=N)
+        _run_adapters(handle, mode, 1024, N, 1024, 8, [1] * N, list(rng.randint(-1, 6, N)), 6, seed=N, beta=1.0)
+
+
+def test_adapters_where_there_is_nothing(handle):
+    for mode in MODES:
+        _run_adapters(handle, mode, 100, 50, 60, 8, [], [], 2)                      # no groups
+        _run_adapters(handle, mode, 100, 50, 60, 8, [20, 30], [0, 1], 0)            # no adapters
+        _run_adapters(handle, mode, 100, 50, 60, 0, [20, 30], [0, 1], 2)            # no rank
+        _run_adapters(handle, mode, 100, 50, 60, 8, [20, 30], [7, -3], 2)           # none that exists
+        _run_adapters(handle, mode, 100, 50, 60, 8, [20, 30], [1, 0], 2, alpha=0.0, beta=1.0)
+        _run_adapters(handle, mode, 100, 50, 60, 8, [20, 30], [1, 0], 2, scales=False)
+        _run_adapters(handle, mode, 100, 50, 0, 8, [20, 30], [1, 0], 2, beta=1.0)   # no depth
+    _run_adapters(handle, "bf16", 140, 200, 300, 16, [150, 40], [1, 0], 2, wide=True)
+
+
+def test_columns_without_depth_or_alpha(handle):
+    """C <- beta C in the groups' columns, and A and B are not read."""
+    import torch
+    ec = _ec()
+    for K, alpha in ((0, 1.0), (40, 0.0)):
+        for beta in (0.0, 0.5):
+            C = Field(30, 20, fill=7.0, values=torch.randn((1, 20, 30), device="cuda"))
+            want = C.view().clone()
+            want[0, 3:15] = want[0, 3:15] * beta
+            handle.sgemm_grouped(ec.OP_T, ec.OP_N, 2, 30, 20, K, alpha, None, 0, 0, None, 0, _offsets([5, 7], 3), beta, C.ptr(), C.ld,
+                                 ec.MODE_FP16_SPLIT)
+            torch.cuda.synchronize()
+            assert torch.equal(C.view(), want)
+            C = Field(30, 20, count=2, fill=7.0, values=torch.randn((2, 20, 30), device="cuda"))
+            want = C.view() * beta
+            handle.sgemm_grouped_depth(ec.OP_N, ec.OP_T, 2, 30, 20, K, alpha, None, 0, None, 0, _offsets([5, 7], 3), beta, C.ptr(), C.ld,
+                                       C.stride, ec.MODE_BF16_FULL)
+            torch.cuda.synchronize()
+            assert torch.equal(C.view(), want)
+
+
+@pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("trans", ["TN", "NT"])
+def test_values_that_are_not_finite_stay_in_their_rows_and_columns(handle, trans, mode):
+    """An infinity, a NaN and the largest numbers: what they meet may be infinite or NaN, or saturated in FP16 mode; the rest
+    is as without them, bit for bit, also what is added to C."""
+    import torch
+    ec, gen = _ec(), _gen(9)
+    M, N, K, sizes = 300, 400, 200, [150, 250]
+    a_shape = (M, K) if trans[0] == "N" else (K, M)
+    b_shape = (K, N) if trans[1] == "N" else (N, K)
+    A, B = Field(*a_shape, count=2, gen=gen), Field(*b_shape, gen=gen)
+    results = []
+    for spoilt in (False, True):
+        a = A.view() if trans[0] == "T" else A.view().transpose(1, 2)      # [g, m, k]
+        b = B.view()[0] if trans[1] == "N" else B.view()[0].t()            # [n, k]
+        if spoilt:
+            a[0, 17, 33] = float("inf")
+            a[1, 290, 7] = float("nan")
+            b[260, 100] = 3.0e38
+            b[399, 199] = -float("inf")
+        C = Field(M, N, values=torch.full((1, N, M), 0.25, device="cuda"), fill=7.0)
+        handle.sgemm_grouped(_ops(trans[0]), _ops(trans[1]), 2, M, N, K, 1.0, A.ptr(), A.ld, A.stride, B.ptr(), B.ld, _offsets(sizes), 2.0,
+                             C.ptr(), C.ld, _mode(mode))
+        torch.cuda.synchronize()
+        results.append(C.view()[0].clone())     # [n, m]
+    clean, spoilt = results
+    touched = torch.zeros_like(clean, dtype=torch.bool)
+    touched[:150, 17] = touched[150:, 290] = touched[260] = touched[399] = True
+    assert torch.equal(clean[~touched], spoilt[~touched])
+    assert not bool(torch.isfinite(spoilt[:150, 17]).any())
+    assert bool(torch.isnan(spoilt[150:, 290]).all())
+    assert not bool(torch.isfinite(spoilt[399]).any())
+    if mode == "fp16":      # saturated, not infinite
+        assert bool(torch.isfinite(spoilt[260][torch.arange(M, device="cuda") != 290]).all())
+
+
+def test_offsets_that_no_program_should_pass(handle):
+    """Negative, decreasing and far too large offsets: no answer is promised, but nothing outside C is written."""
+    import torch
+    ec, gen = _ec(), _gen(2)
+    M, N, K = 200, 300, 90
+    bad = [[-5, 100, 50, 400], [300, 0, 300, 0], [1 << 40, -(1 << 40), 1 << 62, 0], [0, 300, 0, 300], [299, 299, 1 << 33, 3]]
+    for offsets in bad:
+        offs = torch.tensor(offsets, dtype=torch.int64, device="cuda")
+        A, B, C = Field(K, M, count=3, gen=gen), Field(K, N, gen=gen), Field(M, N, pad=4, fill=7.0)
+        handle.sgemm_grouped(ec.OP_T, ec.OP_N, 3, M, N, K, 1.0, A.ptr(), A.ld, A.stride, B.ptr(), B.ld, offs, 0.0, C.ptr(), C.ld,
+                             ec.MODE_FP16_SPLIT)
+        torch.cuda.synchronize()
+        C.view().fill_(7.0)
+        assert bool((C.store == 7.0).all())
+        X, G, W = Field(M, N, gen=gen), Field(K, N, gen=gen), Field(M, K, count=3, fill=7.0, pad=1)
+        handle.sgemm_grouped_depth(ec.OP_N, ec.OP_T, 3, M, K, N, 1.0, X.ptr(), X.ld, G.ptr(), G.ld, offs, 0.0, W.ptr(), W.ld, W.stride,
+                                   ec.MODE_BF16_FULL)
+        torch.cuda.synchronize()
+        W.view().fill_(7.0)
+        assert bool((W.store == 7.0).all())
+        D, U, P, H = Field(K, 8, count=2, gen=gen), Field(8, M, count=2, gen=gen), Field(K, M, gen=gen), Field(8, N, fill=7.0)
+        handle.sgemm_adapters(ec.OP_T, ec.OP_N, M, N, K, 1.0, P.ptr(), P.ld, B.ptr(), B.ld, 3, offs,
+                              torch.tensor([0, 1 << 30, 1], dtype=torch.int32, device="cuda"), 2, 8, ec.OP_T, D.ptr(), D.ld, D.stride, ec.OP_T,
+                              U.ptr(), U.ld, U.stride, None, H.ptr(), H.ld, 0.0, C.ptr(), C.ld, ec.MODE_FP16_SPLIT)
+        torch.cuda.synchronize()
+        C.view().fill_(7.0), H.view().fill_(7.0)
+        assert bool((C.store == 7.0).all()) and bool((H.store == 7.0).all())
+
+
+def test_equal_calls_give_equal_bits_on_any_stream(handle):
+    import torch
+    first = _run_columns(handle, "TN", "fp16", 300, 700, [100, 5, 300], seed=5).store.clone()
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    other = _ec().Handle()
+    other.set_stream(stream.cuda_stream)
+    with torch.cuda.stream(stream):
+        again = _run_columns(other, "TN", "fp16", 300, 700, [100, 5, 300], seed=5).store.clone()
+    torch.cuda.synchronize()
+    other.destroy()
+    assert torch.equal(first, again)
+
+
+def test_captured_calls_replay_with_the_offsets_of_the_day():
+    """A graph of a layer of experts, forward and backward, and of a projection with adapters."""
+    import torch
+    ec, gen = _ec(), _gen(6)
+    E, T, K, M, R = 4, 300, 160, 190, 8
+    x, g = torch.randn((T, K), generator=gen, device="cuda"), torch.randn((T, M), generator=gen, device="cuda")
+    W = torch.randn((E, M, K), generator=gen, device="cuda")
+    D, U = torch.randn((3, R, K), generator=gen, device="cuda"), torch.randn((3, M, R), generator=gen, device="cuda")
+    offs, index = torch.zeros(E + 1, dtype=torch.int64, device="cuda"), torch.zeros(E, dtype=torch.int32, device="cuda")
+    outs = [torch.zeros((T, M), device="cuda"), torch.zeros((T, K), device="cuda"), torch.zeros((E, M, K), device="cuda"),
+            torch.zeros((T, M), device="cuda"), torch.zeros((T, R), device="cuda")]
+
+    def calls(h, y, dx, dw, z, hid):
+        h.sgemm_grouped(ec.OP_T, ec.OP_N, E, M, T, K, 1.0, W, K, M * K, x, K, offs, 0.0, y, M, ec.MODE_FP16_SPLIT)
+        h.sgemm_grouped(ec.OP_N, ec.OP_N, E, K, T, M, 1.0, W, K, M * K, g, M, offs, 0.0, dx, K, ec.MODE_FP16_SPLIT)
+        h.sgemm_grouped_depth(ec.OP_N, ec.OP_T, E, K, M, T, 1.0, x, K, g, M, offs, 0.0, dw, K, M * K, ec.MODE_BF16_FULL)
+        h.sgemm_adapters(ec.OP_T, ec.OP_N, M, T, K, 1.0, W, K, x, K, E, offs, index, 3, R, ec.OP_T, D, K, R * K, ec.OP_T, U, R, M * R, None,
+                         hid, R, 0.0, z, M, ec.MODE_FP16_SPLIT)
+
+    captured, eager = ec.Handle(), ec.Handle()
+    eager.set_stream(torch.cuda.current_stream().cuda_stream)
+    nbytes = max(256, captured.workspace_size(ec.OP_T, ec.OP_N, M, T, K, ec.MODE_FP16_SPLIT))
+    workspace = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+    captured.set_workspace(workspace, nbytes)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured.set_stream(torch.cuda.current_stream().cuda_stream)
+        calls(captured, *outs)
+    for sizes, ids in (([100, 0, 150, 50], [0, 1, 2, 0]), ([1, 1, 1, 1], [2, -1, 0, 0]), ([0, 0, 0, 300], [1, 1, 1, 1]), ([75] * 4, [0, 5, 2, 1])):
+        offs.copy_(_offsets(sizes)), index.copy_(torch.tensor(ids, dtype=torch.int32, device="cuda"))
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        want = [torch.zeros_like(o) for o in outs]
+        calls(eager, *want)
+        torch.cuda.synchronize()
+        for o, w in zip(outs, want):
+            assert torch.equal(o, w)
+    captured.destroy(), eager.destroy()
+
+
+def test_a_layer_of_experts_forward_and_backward(handle):
+    """y = W2[e] relu(W1[e] x): the program's calls one after the other, against autograd in 64 bits and against differences."""
+    import torch
+    ec, gen = _ec(), _gen(11)
+    E, T, K, F, M = 5, 230, 96, 160, 72
+    sizes, mode = [60, 0, 1, 100, 69], ec.MODE_FP16_SPLIT
+    offs = _offsets(sizes)
+    x = torch.randn((T, K), generator=gen, device="cuda")
+    W1, W2 = torch.randn((E, F, K), generator=gen, device="cuda") / K ** 0.5, torch.randn((E, M, F), generator=gen, device="cuda") / F ** 0.5
+    gy = torch.randn((T, M), generator=gen, device="cuda")
+
+    def up(W, rows, width, out):    # rows of `width` times W[e]^T
+        n = W.shape[1]
+        handle.sgemm_grouped(ec.OP_T, ec.OP_N, E, n, T, width, 1.0, W, width, n * width, rows, width, offs, 0.0, out, n, mode)
+        return out
+
+    def back(W, rows, out):
+        n, width = W.shape[1], W.shape[2]
+        handle.sgemm_grouped(ec.OP_N, ec.OP_N, E, width, T, n, 1.0, W, width, n * width, rows, n, offs, 0.0, out, width, mode)
+        return out
+
+    def weights(rows, grads, out):
+        n, width = grads.shape[1], rows.shape[1]
+        handle.sgemm_grouped_depth(ec.OP_N, ec.OP_T, E, width, n, T, 1.0, rows, width, grads, n, offs, 0.0, out, width, n * width, mode)
+        return out
+
+    h = up(W1, x, K, torch.empty((T, F), device="cuda"))
+    a = h.relu()
+    y = up(W2, a, F, torch.empty((T, M), device="cuda"))
+    ga = back(W2, gy, torch.empty((T, F), device="cuda"))
+    gW2 = weights(a, gy, torch.empty_like(W2))
+    gh = ga * (h > 0)
+    gx = back(W1, gh, torch.empty((T, K), device="cuda"))
+    gW1 = weights(x, gh, torch.empty_like(W1))
+    torch.cuda.synchronize()
+
+    def layer(x, W1, W2):
+        out, at = [], 0
+        for e, n in enumerate(sizes):
+            out.append((x[at:at + n] @ W1[e].t()).relu() @ W2[e].t())
+            at += n
+        return torch.cat(out)
+
+    leaves = [v.cpu().double().requires_grad_() for v in (x, W1, W2)]
+    want = layer(*leaves)
+    grads = torch.autograd.grad((want * gy.cpu().double()).sum(), leaves)
+    for got, ref in zip((y, gx, gW1, gW2), (want, *grads)):
+        off = float((got.cpu().double() - ref.detach()).norm() / ref.detach().norm())
+        # two products after each other, each off by at most 2^-21 + 11 (16 2^-25 + 2^-24) of S; in the 2-norm S is at most
+        # sqrt(depth) times the result's for independent values, and errors of independent elements add up as their root
+        # does: 2 sqrt(160) 6.4e-6 / sqrt(160)
+        assert off < 1.3e-5, off
+    # one difference along a random direction, in 64 bits: <grad, d> against (f(v + d) - f(v - d)) / 2; relu's corners are not met
+    # by steps this small but for a few of the 36800 values
+    for i, got in ((0, gx), (1, gW1), (2, gW2)):
+        v = [l.detach() for l in leaves]
+        d = 1e-7 * torch.randn(v[i].shape, dtype=torch.float64)
+        f = lambda sign: (layer(*[u + sign * d if k == i else u for k, u in enumerate(v)]) * gy.cpu().double()).sum()  # noqa: E731
+        difference, along = float(f(1.0) - f(-1.0)) / 2, float((got.cpu().double() * d).sum())
+        assert abs(difference - along) <= 1e-3 * float(got.double().norm()) * float(d.norm()) / d.numel() ** 0.5 + 1e-9
+
+
+def test_adapters_forward_and_backward(handle):
+    """A projection with an adapter per task: forward, and the gradients of the input and of the adapters."""
+    import torch
+    ec, gen = _ec(), _gen(12)
+    T, K, M, R = 210, 120, 88, 8
+    sizes, mode = [50, 60, 100], ec.MODE_FP16_SPLIT
+    offs, index = _offsets(sizes), torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda")
+    x, gy = torch.randn((T, K), generator=gen, device="cuda"), torch.randn((T, M), generator=gen, device="cuda")
+    W = torch.randn((M, K), generator=gen, device="cuda") / K ** 0.5
+    D, U = torch.randn((3, R, K), generator=gen, device="cuda") / K ** 0.5, torch.randn((3, M, R), generator=gen, device="cuda") / R ** 0.5
+    scale = 2.0
+    scales = torch.full((3,), scale, device="cuda")
+    y, H = torch.empty((T, M), device="cuda"), torch.empty((T, R), device="cuda")
+    gx, gH = torch.empty((T, K), device="cuda"), torch.empty((T, R), device="cuda")
+    gD, gU = torch.empty_like(D), torch.empty_like(U)
+    handle.sgemm_adapters(ec.OP_T, ec.OP_N, M, T, K, 1.0, W, K, x, K, 3, offs, index, 3, R, ec.OP_T, D, K, R * K, ec.OP_T, U, R, M * R, scales,
+                          H, R, 0.0, y, M, mode)
+    handle.sgemm_adapters(ec.OP_N, ec.OP_N, K, T, M, 1.0, W, K, gy, M, 3, offs, index, 3, R, ec.OP_N, U, R, M * R, ec.OP_N, D, K, R * K, scales,
+                          gH, R, 0.0, gx, K, mode)
+    handle.sgemm_grouped_depth(ec.OP_N, ec.OP_T, 3, K, R, T, scale, x, K, gH, R, offs, 0.0, gD, K, R * K, mode)
+    handle.sgemm_grouped_depth(ec.OP_N, ec.OP_T, 3, R, M, T, scale, H, R, gy, M, offs, 0.0, gU, R, M * R, mode)
+    torch.cuda.synchronize()
+    leaves = [v.cpu().double().requires_grad_() for v in (x, D, U)]
+    out, at = [], 0
+    for e, n in enumerate(sizes):
+        rows = leaves[0][at:at + n]
+        out.append(rows @ W.cpu().double().t() + scale * (rows @ leaves[1][e].t()) @ leaves[2][e].t())
+        at += n
+    want = torch.cat(out)
+    grads = torch.autograd.grad((want * gy.cpu().double()).sum(), leaves)
+    for got, ref in zip((y, gx, gD, gU), (want, *grads)):
+        off = float((got.cpu().double() - ref.detach()).norm() / ref.detach().norm())
+        assert off < 1.3e-5, off    # as for the layer of experts
+
+
+def test_refusals(handle):
+    """Whatever is wrong with a call: the status, which argument, and nothing enqueued."""
+    import torch
+    ec = _ec()
+    t = torch.zeros(4096, device="cuda")
+    offs, index = torch.zeros(4, dtype=torch.int64, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    names = {"sgemm_grouped": "transA transB groups M N K alpha A lda strideA B ldb offsets beta C ldc mode",
+             "sgemm_grouped_depth": "transA transB groups M N K alpha A lda B ldb offsets beta C ldc strideC mode",
+             "sgemm_adapters": "transA transB M N K alpha A lda B ldb groups offsets index adapters rank transD D ldd strideD transU U ldu strideU "
+                               "scales H ldh beta C ldc mode"}
+    sound = dict(transA=ec.OP_T, transB=ec.OP_N, groups=3, M=8, N=8, K=8, alpha=1.0, A=t, lda=8, strideA=64, B=t[1024:], ldb=8, offsets=offs,
+                 beta=0.0, C=t[2048:], ldc=8, strideC=64, mode=ec.MODE_FP16_SPLIT, index=index, adapters=2, rank=4, transD=ec.OP_T, D=t, ldd=8,
+                 strideD=32, transU=ec.OP_T, U=t, ldu=4, strideU=32, scales=None, H=t[3072:], ldh=4)
+    wrong = {name: [dict(transA=2), dict(transB=-1), dict(M=-1), dict(N=-1), dict(K=-1), dict(groups=-1), dict(A=None), dict(lda=7), dict(B=None),
+                    dict(ldb=7), dict(C=None), dict(ldc=7), dict(offsets=None), dict(offsets=offs.data_ptr() + 4), dict(mode=11), dict(mode=-1),
+                    dict(M=1 << 31), dict(N=1 << 31), dict(K=1 << 31, lda=1 << 31, ldb=1 << 31), dict(groups=1 << 31)] for name in names}
+    wrong["sgemm_grouped"] += [dict(strideA=-1), dict(lda=(1 << 21) + 1), dict(ldb=(1 << 21) + 1)]
+    wrong["sgemm_grouped_depth"] += [dict(strideC=63), dict(ldc=1 << 62)]
+    wrong["sgemm_adapters"] += [dict(transD=3), dict(transU=3), dict(rank=-1), dict(rank=1025), dict(adapters=-1), dict(adapters=1 << 31),
+                                dict(index=None), dict(index=index.data_ptr() + 2), dict(D=None), dict(ldd=7), dict(strideD=-1), dict(U=None),
+                                dict(ldu=3), dict(strideU=-1), dict(H=None), dict(ldh=3)]
+    alias = {"ldc": ["ldc", "strideC"]}
+    for name, order in names.items():
+        order = order.split()
+        for change in wrong[name]:
+            with pytest.raises(ec.EcgemmError) as err:
+                getattr(handle, name)(*[{**sound, **change}[k] for k in order])
+            key = next(iter(change))
+            positions = [order.index(k) + 2 for k in alias.get(key, [key]) if k in order]
+            assert err.value.status == ec.ERR_INVALID_ARG and err.value.argument in positions, (name, change, err.value, err.value.argument)
+        for mode in (ec.MODE_AUTO, ec.MODE_FP32_MFMA, ec.MODE_FP16_MARKIDIS):
+            with pytest.raises(ec.EcgemmError) as err:
+                getattr(handle, name)(*[{**sound, "mode": mode}[k] for k in order])
+            assert err.value.status == ec.ERR_UNSUPPORTED
+    torch.cuda.synchronize()
+    assert bool((t == 0).all())
