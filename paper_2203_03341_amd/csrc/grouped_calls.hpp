@@ -62,6 +62,22 @@ ecgemm_status_t launch_grouped(ecgemm_handle_t h, ecgemm_mode_t mode, bool depth
   return ECGEMM_OK;
 }
 
+// The kernels for few columns to a group (narrow_kernel.hpp).
+constexpr int64_t kNarrowMeanColumns = 32, kAdapterDownMeanColumns = 8, kNarrowProjectionColumns = 64;
+int64_t narrow_row_blocks(bool depth_a, int64_t M) { return depth_a ? (M + narrow_rows<true>() - 1) / narrow_rows<true>() : (M + narrow_rows<false>() - 1) / narrow_rows<false>(); }
+bool narrow_fits(bool depth_a, int64_t groups, int64_t M) { return (groups + 1) * narrow_row_blocks(depth_a, M) <= INT_MAX; }
+
+ecgemm_status_t launch_narrow(ecgemm_handle_t h, bool depth_a, bool depth_b, NarrowParams np) {
+  np.row_blocks = (int)narrow_row_blocks(depth_a, np.M);
+  const int64_t groups = np.offsets ? np.groups + (np.clear_outside ? 1 : 0) : 1;
+  static void (*const kernels[2][2])(NarrowParams) = {{narrow_kernel<false, false>, narrow_kernel<false, true>},
+                                                      {narrow_kernel<true, false>, narrow_kernel<true, true>}};
+  void* args[] = {&np};
+  ECGEMM_HIP(h, hipLaunchKernel(reinterpret_cast<const void*>(kernels[depth_a][depth_b]), dim3((unsigned)(groups * np.row_blocks)),
+                                dim3(kNarrowThreads), args, 0, h->stream));
+  return ECGEMM_OK;
+}
+
 // Modes the grouped products run in: those of the method.
 ecgemm_status_t check_grouped_mode(ecgemm_handle_t h, int mode, int position, const char* function) {
   if (!valid_mode_or_auto(mode)) return bad_arg(h, position, (std::string(function) + ": unknown mode").c_str());
@@ -114,6 +130,16 @@ ecgemm_status_t ecgemm_sgemm_grouped(ecgemm_handle_t handle, ecgemm_op_t transA,
   }
   const OnDeviceOf device(h);
   if (device.error != hipSuccess) return hip_fail(h, device.error, "hipSetDevice");
+  if (N <= kNarrowMeanColumns * groups && narrow_fits(transA == ECGEMM_OP_T, groups, M)) {
+    NarrowParams np{};
+    np.A = A, np.lda = lda, np.stride_a = strideA;
+    np.B = B, np.ldb = ldb;
+    np.C = C, np.ldc = ldc;
+    np.M = M, np.N = N, np.K = K;
+    np.offsets = offsets, np.groups = groups;
+    np.alpha = alpha, np.beta = beta;
+    return launch_narrow(h, transA == ECGEMM_OP_T, transB == ECGEMM_OP_N, np);
+  }
   GroupedParams gp{};
   gp.A = A, gp.lda = lda, gp.stride_a = strideA;
   gp.B = B, gp.ldb = ldb;
@@ -234,37 +260,72 @@ ecgemm_status_t ecgemm_sgemm_adapters(ecgemm_handle_t handle, ecgemm_op_t transA
   }
   const OnDeviceOf device(h);
   if (device.error != hipSuccess) return hip_fail(h, device.error, "hipSetDevice");
-  // the shared projection
-  if (M > 0) {
-    st = sgemm_common(h, transA, transB, M, N, K, alpha, A, lda, B, ldb, beta, C, ldc, mode, nullptr, nullptr, kWorkspaceOfHandle);
-    if (st != ECGEMM_OK) return st;
+  const bool depth_b = transB == ECGEMM_OP_N, project = M > 0 && K > 0 && alpha != 0.0f;
+  if (!any) {
+    if (rank > 0) {  // H = 0
+      const dim3 grid((unsigned)((rank + 255) / 256), (unsigned)std::min<int64_t>(N, 65535));
+      hipLaunchKernelGGL(scale_c_kernel, grid, dim3(256), 0, h->stream, rank, N, 0.0f, H, ldh);
+      ECGEMM_HIP(h, hipGetLastError());
+    }
+    if (M == 0) return ECGEMM_OK;
+    return sgemm_common(h, transA, transB, M, N, K, alpha, A, lda, B, ldb, beta, C, ldc, mode, nullptr, nullptr, kWorkspaceOfHandle);
   }
-  if (rank == 0) return ECGEMM_OK;
-  // H = op(D) op(B), zero in every column without an adapter
-  const dim3 grid((unsigned)((rank + 255) / 256), (unsigned)std::min<int64_t>(N, 65535));
-  hipLaunchKernelGGL(scale_c_kernel, grid, dim3(256), 0, h->stream, rank, N, 0.0f, H, ldh);
-  ECGEMM_HIP(h, hipGetLastError());
-  if (!any) return ECGEMM_OK;
-  GroupedParams down{};
-  down.A = D, down.lda = ldd, down.stride_a = strideD;
-  down.B = B, down.ldb = ldb;
-  down.C = H, down.ldc = ldh;
-  down.M = rank, down.N = N, down.K = K;
-  down.offsets = offsets;
-  down.index = index, down.matrices = (int)adapters;
-  down.alpha = 1.0f, down.beta = 0.0f;
-  st = launch_grouped(h, mode, transD == ECGEMM_OP_T, transB == ECGEMM_OP_N, groups, down);
-  if (st != ECGEMM_OK || M == 0) return st;
-  // C += scale op(U) H
-  GroupedParams up{};
-  up.A = U, up.lda = ldu, up.stride_a = strideU;
-  up.B = H, up.ldb = ldh;
+  // H = op(D) op(B), zero in every column without an adapter: few columns to a group, the adapters are read once, else B is
+  if (N < kAdapterDownMeanColumns * groups && narrow_fits(transD == ECGEMM_OP_T, groups, rank)) {
+    NarrowParams down{};
+    down.A = D, down.lda = ldd, down.stride_a = strideD;
+    down.B = B, down.ldb = ldb;
+    down.C = H, down.ldc = ldh;
+    down.M = rank, down.N = N, down.K = K;
+    down.offsets = offsets, down.groups = groups;
+    down.index = index, down.matrices = (int)adapters;
+    down.alpha = 1.0f, down.beta = 0.0f;
+    down.clear_outside = 1;
+    st = launch_narrow(h, transD == ECGEMM_OP_T, depth_b, down);
+    if (st != ECGEMM_OK) return st;
+  } else {
+    AdapterDownParams down{};
+    down.B = B, down.ldb = ldb;
+    down.D = D, down.ldd = ldd, down.stride_d = strideD;
+    down.N = N, down.K = K, down.rank = rank;
+    down.offsets = offsets, down.groups = groups;
+    down.index = index, down.matrices = (int)adapters;
+    down.H = H, down.ldh = ldh;
+    static void (*const kernels[2][2])(AdapterDownParams) = {{adapter_down_kernel<false, false>, adapter_down_kernel<false, true>},
+                                                             {adapter_down_kernel<true, false>, adapter_down_kernel<true, true>}};
+    void* args[] = {&down};
+    ECGEMM_HIP(h, hipLaunchKernel(reinterpret_cast<const void*>(kernels[depth_b][transD == ECGEMM_OP_T]), dim3((unsigned)narrow_row_blocks(depth_b, N)),
+                                  dim3(kNarrowThreads), args, 0, h->stream));
+  }
+  if (M == 0) return ECGEMM_OK;
+  if (project && N <= kNarrowProjectionColumns && lda <= kGroupedLargestLd) {
+    // few columns: the projection reads its matrix once, and adds the adapters to what it writes
+    NarrowParams np{};
+    np.A = A, np.lda = lda;
+    np.B = B, np.ldb = ldb;
+    np.C = C, np.ldc = ldc;
+    np.M = M, np.N = N, np.K = K;
+    np.alpha = alpha, np.beta = beta;
+    np.U = U, np.ldu = ldu, np.stride_u = strideU, np.rank = rank, np.u_depth = transU == ECGEMM_OP_T;
+    np.H = H, np.ldh = ldh, np.scales = scales;
+    np.adapter_offsets = offsets, np.adapter_groups = groups, np.index = index, np.matrices = (int)adapters;
+    return launch_narrow(h, transA == ECGEMM_OP_T, depth_b, np);
+  }
+  // C = scales op(U) H + beta C first, which the projection adds to as it writes: it finds what it reads in the caches
+  AdapterUpParams up{};
+  up.U = U, up.ldu = ldu, up.stride_u = strideU;
+  up.H = H, up.ldh = ldh;
   up.C = C, up.ldc = ldc;
-  up.M = M, up.N = N, up.K = rank;
-  up.offsets = offsets;
-  up.index = index, up.matrices = (int)adapters, up.scales = scales;
-  up.alpha = 1.0f, up.beta = 1.0f;
-  return launch_grouped(h, mode, transU == ECGEMM_OP_T, true, groups, up);
+  up.M = M, up.N = N, up.rank = rank;
+  up.offsets = offsets, up.groups = groups;
+  up.index = index, up.matrices = (int)adapters;
+  up.scales = scales, up.beta = beta;
+  up.row_blocks = (int)((M + 255) / 256);
+  hipLaunchKernelGGL((transU == ECGEMM_OP_T ? adapter_up_kernel<true> : adapter_up_kernel<false>),
+                     dim3((unsigned)(up.row_blocks * ((N + kNarrowColumns - 1) / kNarrowColumns))), dim3(256), 0, h->stream, up);
+  ECGEMM_HIP(h, hipGetLastError());
+  if (!project) return ECGEMM_OK;
+  return sgemm_common(h, transA, transB, M, N, K, alpha, A, lda, B, ldb, 1.0f, C, ldc, mode, nullptr, nullptr, kWorkspaceOfHandle);
 }
 
 }  // extern "C"

@@ -7,6 +7,7 @@
 #pragma once
 #include "fused_kernel.hpp"
 #include "grouped_kernel.hpp"
+#include "narrow_kernel.hpp"
 #include "product_kernel.hpp"
 #include "split_kernels.hpp"
 #include "wide_kernel.hpp"
@@ -79,6 +80,11 @@ typedef ProductConfig<kMethodFp32, 256, 128, 128, 64, 2, 3, 1> Fp32Config;
 #else
 #define ECGEMM_GROUPED_BF16_GROUP extern
 #endif
+#ifdef ECGEMM_INSTANTIATE_NARROW
+#define ECGEMM_NARROW_GROUP
+#else
+#define ECGEMM_NARROW_GROUP extern
+#endif
 #ifdef ECGEMM_INSTANTIATE_SPLIT
 #define ECGEMM_SPLIT_GROUP
 #else
@@ -144,6 +150,17 @@ ECGEMM_GROUPED_KERNELS_OF(ECGEMM_GROUPED_FP16_GROUP, kMethodFp16Split, false)
 ECGEMM_GROUPED_KERNELS_OF(ECGEMM_GROUPED_FP16_GROUP, kMethodFp16Split, true)  // for handles with a pre-scaling
 ECGEMM_GROUPED_KERNELS_OF(ECGEMM_GROUPED_BF16_GROUP, kMethodBf16Full, false)
 ECGEMM_GROUPED_KERNELS_OF(ECGEMM_GROUPED_BF16_GROUP, kMethodBf16Full, true)
+
+ECGEMM_NARROW_GROUP template __global__ void narrow_kernel<false, false>(const NarrowParams);
+ECGEMM_NARROW_GROUP template __global__ void narrow_kernel<false, true>(const NarrowParams);
+ECGEMM_NARROW_GROUP template __global__ void narrow_kernel<true, false>(const NarrowParams);
+ECGEMM_NARROW_GROUP template __global__ void narrow_kernel<true, true>(const NarrowParams);
+ECGEMM_NARROW_GROUP template __global__ void adapter_down_kernel<false, false>(const AdapterDownParams);
+ECGEMM_NARROW_GROUP template __global__ void adapter_down_kernel<false, true>(const AdapterDownParams);
+ECGEMM_NARROW_GROUP template __global__ void adapter_down_kernel<true, false>(const AdapterDownParams);
+ECGEMM_NARROW_GROUP template __global__ void adapter_down_kernel<true, true>(const AdapterDownParams);
+ECGEMM_NARROW_GROUP template __global__ void adapter_up_kernel<false>(const AdapterUpParams);
+ECGEMM_NARROW_GROUP template __global__ void adapter_up_kernel<true>(const AdapterUpParams);
 
 #define ECGEMM_SPLIT_KERNELS_OF(KIND)                                                                     \
   ECGEMM_SPLIT_GROUP template __global__ void split_kernel<KIND, kSplitKContiguous, false>(const SplitJob);      \
