@@ -60,6 +60,14 @@ struct GroupedItem {
   float alpha;
 };
 
+// the value of the first lane, for what is the same in all of them
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+  const unsigned low = (unsigned)__builtin_amdgcn_readfirstlane((int)v), high = (unsigned)__builtin_amdgcn_readfirstlane((int)(v >> 32));
+  return (int64_t)(((uint64_t)high << 32) | low);
+}
+__device__ __forceinline__ const float* uniform(const float* v) { return reinterpret_cast<const float*>(uniform((int64_t)(uintptr_t)v)); }
+
 // One operand of a tile, as WideOperand but for any number of rows and either mode.  A splitting thread t of 256 holds UNITS
 // units of a row and an octet of the depth each:
 //   !DEPTH (rows contiguous)   rows UNITS (t % (128 / UNITS)) + u, octet t / (128 / UNITS); load j: k = 8 octet + j of all rows
@@ -73,6 +81,9 @@ struct GroupedOperand {
   typedef unsigned uint4_t __attribute__((ext_vector_type(4)));
   typedef float unit_rows_t __attribute__((ext_vector_type(UNITS), aligned(4)));
   typedef float float4_any_t __attribute__((ext_vector_type(4), aligned(4)));
+  // (what went through uniform() is no longer known to be global memory, and would be read by FLAT instructions)
+  typedef __attribute__((address_space(1))) unit_rows_t global_rows_t;
+  typedef __attribute__((address_space(1))) float4_any_t global_float4_t;
 
   const float* first;  // &X(first row of the tile, first k), the same for the block
   int64_t ld, K;
@@ -93,7 +104,9 @@ struct GroupedOperand {
 
   __device__ __forceinline__ void init(const float* first_, int64_t ld_, int64_t K_, int exist, int readable, float factor_, int t) {
     asm volatile("" : "+v"(t));  // (or everything made of it is worked out before the first tile and kept)
-    first = first_, ld = ld_, K = K_, factor = factor_;
+    // (a buffer load takes its base from scalar registers: where the compiler cannot tell that it is the same in all lanes, every
+    // load becomes a loop over them)
+    first = uniform(first_), ld = ld_, K = uniform(K_), factor = factor_;
     octet = DEPTH ? t % OCTETS : t / (kGroupedTile / UNITS);
     row = DEPTH ? t / OCTETS : UNITS * (t % (kGroupedTile / UNITS));
     rows = DEPTH ? exist : readable;
@@ -141,26 +154,26 @@ struct GroupedOperand {
 #pragma unroll
         for (int j = 0; j < 2 * UNITS; ++j) {
           const int64_t k = k0 + 4 * (j & 1);
-          const float4_any_t v = *reinterpret_cast<const float4_any_t*>(first + clamped_row(j >> 1) * ld + (k < K - 4 ? k : K - 4));
+          const float4_any_t v = *(const global_float4_t*)(first + clamped_row(j >> 1) * ld + (k < K - 4 ? k : K - 4));
 #pragma unroll
           for (int e = 0; e < 4; ++e) x[8 * (j >> 1) + 4 * (j & 1) + e] = v[e];
         }
       } else {
 #pragma unroll
-        for (int i = 0; i < VALUES; ++i) x[i] = first[clamped_row(i >> 3) * ld + (k0 + (i & 7) < K ? k0 + (i & 7) : K - 1)];
+        for (int i = 0; i < VALUES; ++i) x[i] = load_global(first + clamped_row(i >> 3) * ld + (k0 + (i & 7) < K ? k0 + (i & 7) : K - 1));
       }
     } else {
       if (!straddles) {
         const int start = row + UNITS <= rows ? row : rows - UNITS;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const unit_rows_t v = *reinterpret_cast<const unit_rows_t*>(first + start + (k0 + j < K ? k0 + j : K - 1) * ld);
+          const unit_rows_t v = *(const global_rows_t*)(first + start + (k0 + j < K ? k0 + j : K - 1) * ld);
 #pragma unroll
           for (int u = 0; u < UNITS; ++u) x[8 * u + j] = v[u];
         }
       } else {
 #pragma unroll
-        for (int i = 0; i < VALUES; ++i) x[i] = first[clamped_row(i >> 3) + (k0 + (i & 7) < K ? k0 + (i & 7) : K - 1) * ld];
+        for (int i = 0; i < VALUES; ++i) x[i] = load_global(first + clamped_row(i >> 3) + (k0 + (i & 7) < K ? k0 + (i & 7) : K - 1) * ld);
       }
     }
   }
@@ -295,13 +308,6 @@ __device__ __forceinline__ void make_group_table(const GroupedParams& p, GroupTa
     for (int i = 0; i < 64; ++i) table.first_tile[kGroupsPerLaunch + i] = at;
   }
   __syncthreads();
-}
-
-// the value of the first lane, for what is the same in all of them
-__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-__device__ __forceinline__ int64_t uniform(int64_t v) {
-  const unsigned low = (unsigned)__builtin_amdgcn_readfirstlane((int)v), high = (unsigned)__builtin_amdgcn_readfirstlane((int)(v >> 32));
-  return (int64_t)(((uint64_t)high << 32) | low);
 }
 
 template <int METHOD, bool DEPTH_A, bool DEPTH_B, bool SCALED>
