@@ -24,8 +24,8 @@ struct OnDeviceOf {
 typedef void (*grouped_fn_t)(GroupedParams);
 template <int METHOD, bool SCALED>
 grouped_fn_t grouped_kernel_of(bool depth_a, bool depth_b) {
-  return depth_a ? (depth_b ? grouped_kernel<METHOD, true, true, SCALED> : grouped_kernel<METHOD, true, false, SCALED>)
-                 : (depth_b ? grouped_kernel<METHOD, false, true, SCALED> : grouped_kernel<METHOD, false, false, SCALED>);
+  return depth_a ? (depth_b ? grouped_kernel<METHOD, true, true, SCALED, false> : grouped_kernel<METHOD, true, false, SCALED, false>)
+                 : (depth_b ? grouped_kernel<METHOD, false, true, SCALED, false> : grouped_kernel<METHOD, false, false, SCALED, false>);
 }
 
 constexpr int64_t kGroupedMostTiles = 1 << 30;
@@ -51,8 +51,7 @@ ecgemm_status_t launch_grouped(ecgemm_handle_t h, ecgemm_mode_t mode, bool depth
   for (int64_t first = 0; first < groups; first += kGroupsPerLaunch) {
     gp.groups = (int)std::min<int64_t>(groups - first, kGroupsPerLaunch);
     gp.offsets = whole.offsets + first;
-    if (whole.index) gp.index = whole.index + first;
-    else gp.A = whole.A + first * whole.stride_a;
+    gp.A = whole.A + first * whole.stride_a;
     gp.C = whole.C + first * whole.stride_c;
     const int64_t tiles = most_grouped_tiles(gp.along_depth, gp.groups, gp.M, gp.N);
     const int64_t grid = std::max(std::min<int64_t>(tiles, h->compute_units), (tiles + kGroupedTilesPerBlock - 1) / kGroupedTilesPerBlock);
@@ -64,16 +63,25 @@ ecgemm_status_t launch_grouped(ecgemm_handle_t h, ecgemm_mode_t mode, bool depth
 
 // The kernels for few columns to a group (narrow_kernel.hpp).
 constexpr int64_t kNarrowMeanColumns = 32, kAdapterDownMeanColumns = 8, kNarrowProjectionColumns = 64;
-int64_t narrow_row_blocks(bool depth_a, int64_t M) { return depth_a ? (M + narrow_rows<true>() - 1) / narrow_rows<true>() : (M + narrow_rows<false>() - 1) / narrow_rows<false>(); }
-bool narrow_fits(bool depth_a, int64_t groups, int64_t M) { return (groups + 1) * narrow_row_blocks(depth_a, M) <= INT_MAX; }
+constexpr int64_t kNarrowTallBlocks = 256;
+constexpr int64_t kAdapterOneLaunchDepth = 8192, kAdapterOneLaunchChunks = 8;
+// Blocks of 16 rows the operand that is read once is taken in: four where its rows are contiguous, else two where that leaves
+// enough blocks and there are enough columns for it to matter.
+int narrow_fr(bool depth, int64_t groups, int64_t rows, int64_t columns) {
+  return !depth ? 4 : columns > 16 && groups * ((rows + 31) / 32) >= kNarrowTallBlocks ? 2 : 1;
+}
+int64_t narrow_row_blocks(int fr, int64_t rows) { return (rows + 16 * fr - 1) / (16 * fr); }
+bool narrow_fits(int64_t groups, int64_t M) { return (groups + 1) * narrow_row_blocks(1, M) <= INT_MAX; }
 
 ecgemm_status_t launch_narrow(ecgemm_handle_t h, bool depth_a, bool depth_b, NarrowParams np) {
-  np.row_blocks = (int)narrow_row_blocks(depth_a, np.M);
-  const int64_t groups = np.offsets ? np.groups + (np.clear_outside ? 1 : 0) : 1;
-  static void (*const kernels[2][2])(NarrowParams) = {{narrow_kernel<false, false>, narrow_kernel<false, true>},
-                                                      {narrow_kernel<true, false>, narrow_kernel<true, true>}};
+  const int64_t groups = np.offsets ? np.groups : 1;
+  const int fr = narrow_fr(depth_a, groups, np.M, np.N / groups);
+  np.row_blocks = (int)narrow_row_blocks(fr, np.M);
+  void (*const kernel)(NarrowParams) = fr == 4   ? (depth_b ? narrow_kernel<false, true, 4> : narrow_kernel<false, false, 4>)
+                                       : fr == 2 ? (depth_b ? narrow_kernel<true, true, 2> : narrow_kernel<true, false, 2>)
+                                                 : (depth_b ? narrow_kernel<true, true, 1> : narrow_kernel<true, false, 1>);
   void* args[] = {&np};
-  ECGEMM_HIP(h, hipLaunchKernel(reinterpret_cast<const void*>(kernels[depth_a][depth_b]), dim3((unsigned)(groups * np.row_blocks)),
+  ECGEMM_HIP(h, hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)((groups + (np.clear_outside ? 1 : 0)) * np.row_blocks)),
                                 dim3(kNarrowThreads), args, 0, h->stream));
   return ECGEMM_OK;
 }
@@ -130,7 +138,7 @@ ecgemm_status_t ecgemm_sgemm_grouped(ecgemm_handle_t handle, ecgemm_op_t transA,
   }
   const OnDeviceOf device(h);
   if (device.error != hipSuccess) return hip_fail(h, device.error, "hipSetDevice");
-  if (N <= kNarrowMeanColumns * groups && narrow_fits(transA == ECGEMM_OP_T, groups, M)) {
+  if (N <= kNarrowMeanColumns * groups && narrow_fits(groups, M)) {
     NarrowParams np{};
     np.A = A, np.lda = lda, np.stride_a = strideA;
     np.B = B, np.ldb = ldb;
@@ -271,7 +279,7 @@ ecgemm_status_t ecgemm_sgemm_adapters(ecgemm_handle_t handle, ecgemm_op_t transA
     return sgemm_common(h, transA, transB, M, N, K, alpha, A, lda, B, ldb, beta, C, ldc, mode, nullptr, nullptr, kWorkspaceOfHandle);
   }
   // H = op(D) op(B), zero in every column without an adapter: few columns to a group, the adapters are read once, else B is
-  if (N < kAdapterDownMeanColumns * groups && narrow_fits(transD == ECGEMM_OP_T, groups, rank)) {
+  if (N < kAdapterDownMeanColumns * groups && narrow_fits(groups, rank)) {
     NarrowParams down{};
     down.A = D, down.lda = ldd, down.stride_a = strideD;
     down.B = B, down.ldb = ldb;
@@ -291,10 +299,13 @@ ecgemm_status_t ecgemm_sgemm_adapters(ecgemm_handle_t handle, ecgemm_op_t transA
     down.offsets = offsets, down.groups = groups;
     down.index = index, down.matrices = (int)adapters;
     down.H = H, down.ldh = ldh;
-    static void (*const kernels[2][2])(AdapterDownParams) = {{adapter_down_kernel<false, false>, adapter_down_kernel<false, true>},
-                                                             {adapter_down_kernel<true, false>, adapter_down_kernel<true, true>}};
+    const int fr = narrow_fr(depth_b, 1, N, rank);
+    const bool depth_d = transD == ECGEMM_OP_T;
+    void (*const kernel)(AdapterDownParams) = fr == 4   ? (depth_d ? adapter_down_kernel<false, true, 4> : adapter_down_kernel<false, false, 4>)
+                                              : fr == 2 ? (depth_d ? adapter_down_kernel<true, true, 2> : adapter_down_kernel<true, false, 2>)
+                                                        : (depth_d ? adapter_down_kernel<true, true, 1> : adapter_down_kernel<true, false, 1>);
     void* args[] = {&down};
-    ECGEMM_HIP(h, hipLaunchKernel(reinterpret_cast<const void*>(kernels[depth_b][transD == ECGEMM_OP_T]), dim3((unsigned)narrow_row_blocks(depth_b, N)),
+    ECGEMM_HIP(h, hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)narrow_row_blocks(fr, N), groups > 1 ? 2 : 1),
                                   dim3(kNarrowThreads), args, 0, h->stream));
   }
   if (M == 0) return ECGEMM_OK;
@@ -310,6 +321,32 @@ ecgemm_status_t ecgemm_sgemm_adapters(ecgemm_handle_t handle, ecgemm_op_t transA
     np.H = H, np.ldh = ldh, np.scales = scales;
     np.adapter_offsets = offsets, np.adapter_groups = groups, np.index = index, np.matrices = (int)adapters;
     return launch_narrow(h, transA == ECGEMM_OP_T, depth_b, np);
+  }
+  // Projection and adapters in one launch, where both matrices and H are laid out alike (see grouped_kernel).
+  const int64_t chunk = mode == ECGEMM_MODE_FP16_SPLIT ? 64 : 32, added_chunks = (1 + kGroupedTile * groups / N) * ((rank + chunk - 1) / chunk);
+  const int64_t tiles = tiles_of(M) * tiles_of(N);
+  if (project && transA == transU && depth_b && groups <= kGroupsPerLaunch && lda <= kGroupedLargestLd && ldb <= kGroupedLargestLd &&
+      h->log2_scale_a == 0 && h->log2_scale_b == 0 && K <= kAdapterOneLaunchDepth && added_chunks <= kAdapterOneLaunchChunks) {
+    GroupedParams gp{};
+    gp.A = A, gp.lda = lda;
+    gp.B = B, gp.ldb = ldb;
+    gp.C = C, gp.ldc = ldc;
+    gp.M = M, gp.N = N, gp.K = K;
+    gp.offsets = offsets, gp.groups = (int)groups;
+    gp.index = index, gp.matrices = (int)adapters, gp.scales = scales;
+    gp.tiles_m = (int)tiles_of(M), gp.tiles_n = (int)tiles_of(N);
+    gp.U = U, gp.ldu = ldu, gp.stride_u = strideU, gp.rank = rank;
+    gp.H = H, gp.ldh = ldh;
+    gp.prescale_a = gp.prescale_b = gp.out_scale = 1.0f;
+    gp.alpha = alpha, gp.beta = beta;
+    const bool depth_a = transA == ECGEMM_OP_T;
+    const grouped_fn_t kernel = mode == ECGEMM_MODE_FP16_SPLIT
+                                    ? (depth_a ? grouped_kernel<kMethodFp16Split, true, true, false, true> : grouped_kernel<kMethodFp16Split, false, true, false, true>)
+                                    : (depth_a ? grouped_kernel<kMethodBf16Full, true, true, false, true> : grouped_kernel<kMethodBf16Full, false, true, false, true>);
+    const int64_t grid = std::max(std::min<int64_t>(tiles, h->compute_units), (tiles + kGroupedTilesPerBlock - 1) / kGroupedTilesPerBlock);
+    void* args[] = {&gp};
+    ECGEMM_HIP(h, hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)grid), dim3(kGroupedThreads), args, 0, h->stream));
+    return ECGEMM_OK;
   }
   // C = scales op(U) H + beta C first, which the projection adds to as it writes: it finds what it reads in the caches
   AdapterUpParams up{};

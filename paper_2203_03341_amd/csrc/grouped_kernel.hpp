@@ -36,13 +36,17 @@ struct GroupedParams {
   int64_t M, N, K;   // columns: N is the number of columns of B and C; depth: K is the depth of A and B
   const int64_t* offsets;
   int groups;        // at most kGroupsPerLaunch
-  // columns only, both may be null: which of `matrices` As group g takes (none: the product counts as zero), and a factor
-  // next to alpha for each of them
+  int along_depth;   // 1: groups of the depth, 0: groups of columns
+  int tiles_m, tiles_n;  // tiles_n: not for columns
+  // ADAPTERS only: tiles are of all N columns and tiles_n counts them; group g's columns have scales[a] op(U_a) H added,
+  // a = index[g] if that is one of `matrices` (scales may be null: 1); H is rank x N with the rank contiguous
   const int* index;
   int matrices;
   const float* scales;
-  int along_depth;   // 1: groups of the depth, 0: groups of columns
-  int tiles_m, tiles_n;  // tiles_n: depth only
+  const float* U;
+  int64_t ldu, stride_u, rank;
+  const float* H;
+  int64_t ldh;
   float prescale_a, prescale_b;  // powers of two applied before the split
   float out_scale;               // 1 / (prescale_a prescale_b)
   float alpha, beta;
@@ -57,7 +61,7 @@ struct GroupedItem {
   int64_t K;       // depth, 0 for a group without any (columns: never)
   int rows, cols;  // of the tile that exist, at most 128
   int readable_rows, readable_cols;  // how many are in memory from the first one on, at most 128
-  float alpha;
+  int m0, n0;      // adapters only: the tile's first row and column
 };
 
 // the value of the first lane, for what is the same in all of them
@@ -263,12 +267,16 @@ struct GroupedOperand {
 struct GroupTable {
   int first_tile[kGroupsPerLaunch + 64];  // [groups] and everything behind it: the number of all tiles
   int begin[kGroupsPerLaunch], end[kGroupsPerLaunch];
-  int matrix[kGroupsPerLaunch];  // which A, -1: none
+};
+// ADAPTERS: those of each group's columns.
+struct AdapterTable {
+  int adapter[kGroupsPerLaunch];  // -1: none
+  float scale[kGroupsPerLaunch];
 };
 __device__ __forceinline__ int64_t clamp_offset(int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; }
 // Called by all kGroupedThreads threads; ends with a barrier.  Offsets outside [0, N] or decreasing ones are clamped, so that
 // no tile ever reaches beyond the operands (the caller holds N <= 2^31 - 1).
-__device__ __forceinline__ void make_group_table(const GroupedParams& p, GroupTable& table, int* wave_sums) {
+__device__ __forceinline__ void make_group_table(const GroupedParams& p, GroupTable& table, AdapterTable* adapters, int* wave_sums) {
   constexpr int PER_THREAD = kGroupsPerLaunch / kGroupedThreads;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   int tiles[PER_THREAD], sum = 0;
@@ -279,8 +287,11 @@ __device__ __forceinline__ void make_group_table(const GroupedParams& p, GroupTa
     if (g < p.groups) {
       const int64_t begin = clamp_offset(p.offsets[g], 0, p.N), end = clamp_offset(p.offsets[g + 1], begin, p.N);
       table.begin[g] = (int)begin, table.end[g] = (int)end;
-      const int matrix = p.index != nullptr ? p.index[g] : g;
-      table.matrix[g] = p.index != nullptr && (matrix < 0 || matrix >= p.matrices) ? -1 : matrix;
+      if (adapters != nullptr) {
+        const int a = p.index[g], adapter = a >= 0 && a < p.matrices ? a : -1;
+        adapters->adapter[g] = adapter;
+        adapters->scale[g] = adapter >= 0 && p.scales != nullptr ? p.scales[adapter] : 1.0f;
+      }
       tiles[i] = (int)((end - begin + kGroupedTile - 1) / kGroupedTile);
     }
     sum += tiles[i];  // (at most 2 x 2^24)
@@ -310,8 +321,13 @@ __device__ __forceinline__ void make_group_table(const GroupedParams& p, GroupTa
   __syncthreads();
 }
 
-template <int METHOD, bool DEPTH_A, bool DEPTH_B, bool SCALED>
+// ADAPTERS: a projection of all columns, op(A) op(B), with low-rank adapters.  The groups that a tile's columns belong to add a
+// chunk or two each to its depth: U_a's rows times H's columns, those of other groups taken as zero, times scale / alpha.  C is
+// written once; a pass of its own over C for the adapters costs as much as writing it twice more (4096 cubed, rank 32, 65 us
+// of 440 FP16).
+template <int METHOD, bool DEPTH_A, bool DEPTH_B, bool SCALED, bool ADAPTERS>
 __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_kernel(const GroupedParams p) {
+  static_assert(!ADAPTERS || (DEPTH_B && !SCALED), "H has its rank contiguous");
   constexpr int KIND = split_kind_of(METHOD), NP = parts_of_split(KIND), PRODUCTS = products_of(METHOD), ELEM = element_kind_of(METHOD);
   typedef GroupedOperand<METHOD, DEPTH_A> OperandA;
   typedef GroupedOperand<METHOD, DEPTH_B> OperandB;
@@ -320,6 +336,8 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_kernel(const Group
   typedef typename Mfma<ELEM>::frag_t frag_t;
   __shared__ __attribute__((aligned(1024))) char lds[2 * STAGE_BYTES];
   __shared__ GroupTable table;
+  __shared__ std::conditional_t<ADAPTERS, AdapterTable, char> adapter_space;
+  AdapterTable* const adapter_table = reinterpret_cast<AdapterTable*>(&adapter_space);  // (ADAPTERS only)
   __shared__ int wave_sums[kGroupedThreads / 64];
   // Whether multiplying wave w left its part of the block's tile number i unwritten (below); any[w]: of any tile
   __shared__ __attribute__((aligned(4))) unsigned char not_finite[kGroupedTilesPerBlock][4];
@@ -330,8 +348,11 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_kernel(const Group
   int items;
   if (p.along_depth) {
     items = p.groups * p.tiles_m * p.tiles_n;
+  } else if (ADAPTERS) {
+    make_group_table(p, table, adapter_table, wave_sums);
+    items = p.tiles_m * p.tiles_n;
   } else {
-    make_group_table(p, table, wave_sums);
+    make_group_table(p, table, nullptr, wave_sums);
     const int64_t all = (int64_t)table.first_tile[kGroupsPerLaunch] * p.tiles_m, most = (int64_t)gridDim.x * kGroupedTilesPerBlock;
     items = uniform((int)(all < most ? all : most));
   }
@@ -340,9 +361,18 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_kernel(const Group
 
   auto item_at = [&](int index) {
     GroupedItem it;
-    it.alpha = p.alpha;
     int group, tile_m, tile_n;
-    if (p.along_depth) {
+    if constexpr (ADAPTERS) {
+      tile_coordinates(index, p.tiles_m, p.tiles_n, 4, 1, tile_m, tile_n);
+      const int64_t m0 = (int64_t)tile_m * kGroupedTile, n0 = (int64_t)tile_n * kGroupedTile;
+      it.a = p.A + (DEPTH_A ? m0 * p.lda : m0);
+      it.b = p.B + (DEPTH_B ? n0 * p.ldb : n0);
+      it.c = p.C + m0 + n0 * p.ldc;
+      it.K = p.K;
+      it.rows = it.readable_rows = (int)(p.M - m0 < kGroupedTile ? p.M - m0 : kGroupedTile);
+      it.cols = it.readable_cols = (int)(p.N - n0 < kGroupedTile ? p.N - n0 : kGroupedTile);
+      it.m0 = (int)m0, it.n0 = (int)n0;
+    } else if (p.along_depth) {
       const int tiles = p.tiles_m * p.tiles_n;
       group = index / tiles;
       tile_coordinates(index - group * tiles, p.tiles_m, p.tiles_n, 4, 1, tile_m, tile_n);
@@ -362,25 +392,49 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_kernel(const Group
       group = group < p.groups ? group : p.groups - 1;
       const int begin = uniform(table.begin[group]), end = uniform(table.end[group]);
       const int first_tile = uniform(table.first_tile[group]);
-      const int matrix = uniform(table.matrix[group]);
       const int tiles_n = (end - begin + kGroupedTile - 1) / kGroupedTile;
       const int64_t within = index - (int64_t)first_tile * p.tiles_m;
       // (only offsets that decrease can bring a tile that does not exist: it has no columns and is passed over)
       tile_m = 0, tile_n = tiles_n;
       if (within < (int64_t)tiles_n * p.tiles_m) tile_coordinates((int)within, p.tiles_m, tiles_n, 4, 1, tile_m, tile_n);
       const int64_t m0 = (int64_t)tile_m * kGroupedTile, n0 = begin + (int64_t)tile_n * kGroupedTile;
-      it.a = p.A + matrix * p.stride_a + (DEPTH_A ? m0 * p.lda : m0);
+      it.a = p.A + group * p.stride_a + (DEPTH_A ? m0 * p.lda : m0);
       it.b = p.B + (DEPTH_B ? n0 * p.ldb : n0);
       it.c = p.C + m0 + n0 * p.ldc;
       it.rows = it.readable_rows = (int)(p.M - m0 < kGroupedTile ? p.M - m0 : kGroupedTile);
       it.cols = (int)(end - n0 < kGroupedTile ? end - n0 : kGroupedTile);
       it.readable_cols = (int)(p.N - n0 < kGroupedTile ? p.N - n0 : kGroupedTile);
-      it.K = it.cols > 0 && matrix >= 0 ? p.K : 0;
-      if (p.scales != nullptr && matrix >= 0) it.alpha *= p.scales[matrix];
+      it.K = it.cols > 0 ? p.K : 0;
     }
     return it;
   };
   auto chunks_of = [&](const GroupedItem& it) { return (int)((it.K + CHUNK - 1) / CHUNK); };
+
+  // The adapters of a tile's columns, in the order of their groups: visit(group, first column, last column + 1).
+  const int rank_chunks = ADAPTERS ? (int)((p.rank + CHUNK - 1) / CHUNK) : 0;
+  auto for_adapters = [&](const GroupedItem& it, auto&& visit) {
+    for (int base = 0; base < p.groups; base += 64) {
+      const int g = base + lane;
+      bool hit = false;
+      if (g < p.groups) {
+        const int begin = table.begin[g], end = table.end[g];
+        hit = adapter_table->adapter[g] >= 0 && begin < end && begin < it.n0 + it.cols && end > it.n0;
+      }
+      for (uint64_t left = __builtin_amdgcn_ballot_w64(hit); left != 0; left &= left - 1) {
+        const int at = base + __builtin_ctzll(left);
+        const int lo = uniform(table.begin[at]) - it.n0, hi = uniform(table.end[at]) - it.n0;
+        visit(at, lo > 0 ? lo : 0, hi < it.cols ? hi : it.cols);
+      }
+    }
+  };
+  auto adapters_of = [&](const GroupedItem& it) {
+    int n = 0;
+    for (int base = 0; base < p.groups; base += 64) {
+      const int g = base + lane;
+      n += __popcll(__builtin_amdgcn_ballot_w64(g < p.groups && adapter_table->adapter[g] >= 0 && table.begin[g] < table.end[g] && table.begin[g] < it.n0 + it.cols && table.end[g] > it.n0));
+    }
+    return n;
+  };
 
   auto block_barrier = [&]() {
     __builtin_amdgcn_sched_barrier(0);
@@ -400,13 +454,47 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_kernel(const Group
   // block is through with its tiles it goes through those once more, with Splitter, and writes what was left out.
   if (wave < kGroupedSplitWaves) {
     if constexpr (METHOD == kMethodFp16Split) __builtin_amdgcn_s_setreg(1 | (23 << 6), 1);  // MODE.FP16_OVFL
-    float xa[2][VALUES], xb[2][VALUES];
     OperandA a;
     OperandB b;
+    // The chunks of one group's adapter, from chunk `number` of the tile on.  A tile begins with those: their loads' way is
+    // then covered like that of the projection's first chunk, which is requested before them, by what the multiplying
+    // waves still have to do for the tile before (behind the projection they cost 7 us a tile).
+    auto deposit_adapter = [&](const GroupedItem& it, int group, int lo, int hi, int& number, auto careful_c) {
+      constexpr bool careful = decltype(careful_c)::value;
+      const int adapter = uniform(adapter_table->adapter[group]);
+      const float scale = adapter_table->scale[group];
+      OperandA oa;
+      OperandB ob;
+      float va[VALUES], vb[VALUES];
+      oa.init(p.U + adapter * p.stride_u + (DEPTH_A ? it.m0 * p.ldu : (int64_t)it.m0), p.ldu, p.rank, it.rows, it.readable_rows, 1.0f, t);
+      ob.init(p.H + it.n0 * p.ldh, p.ldh, p.rank, it.cols, it.readable_cols, scale / p.alpha, t);
+      for (int c = 0; c < rank_chunks; ++c, ++number) {
+        char* stage = lds + (number & 1) * STAGE_BYTES;
+        oa.fetch_any(va, c);
+        oa.complete(va, c);
+        if constexpr (careful) oa.deposit_with_care(va, stage);
+        else oa.template deposit<false, false, 0>(va, stage, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        ob.fetch_any(vb, c);
+        ob.complete(vb, c);
+        static_for<VALUES>([&](auto i_c) {
+          constexpr int i = decltype(i_c)::value;
+          const int r = ob.unit_row(i / 8);
+          vb[i] = r >= lo && r < hi ? vb[i] : 0.0f;
+        });
+        if constexpr (careful) {
+          ob.deposit_with_care(vb, stage + REGION_BYTES);
+        } else {
+          ob.template deposit<true, false, 0>(vb, stage + REGION_BYTES, 0);
+        }
+        block_barrier();
+      }
+    };
     for (int index = position; index < items; index += step_items) {
       const GroupedItem it = item_at(index);
       const int chunks = chunks_of(it);
       if (chunks == 0) continue;
+      float xa[2][VALUES], xb[2][VALUES];
       a.init(it.a, p.lda, it.K, it.rows, it.readable_rows, p.prescale_a, t);
       b.init(it.b, p.ldb, it.K, it.cols, it.readable_cols, p.prescale_b, t);
       const int whole = a.straddles || b.straddles ? 0 : (int)(it.K / CHUNK);
@@ -417,6 +505,11 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_kernel(const Group
       };
       request(std::integral_constant<int, 0>{}, 0);
       __builtin_amdgcn_sched_barrier(0);
+      if constexpr (ADAPTERS) {
+        int number = 0;
+        for_adapters(it, [&](int group, int lo, int hi) { deposit_adapter(it, group, lo, hi, number, std::false_type{}); });
+        if (number & 1) block_barrier();
+      }
       request(std::integral_constant<int, 1>{}, 1);
       __builtin_amdgcn_sched_barrier(0);
       int c = 0;
@@ -442,10 +535,11 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_kernel(const Group
             b.template deposit<SCALED, false, 0>(xb[r], lds + r * STAGE_BYTES + REGION_BYTES, 0);
             __builtin_amdgcn_sched_barrier(0);
             request(r_c, c + r + 2);
+            block_barrier();
           }
-          block_barrier();
         });
       }
+      if (chunks & 1) block_barrier();
     }
     block_barrier();  // the multiplying waves' words are there
     if (uniform(any_not_finite[0] | any_not_finite[1] | any_not_finite[2] | any_not_finite[3]) == 0) return;
@@ -453,18 +547,27 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_kernel(const Group
     for (int index = position; index < items; index += step_items, ++number) {
       if (uniform(*reinterpret_cast<const int*>(not_finite[number])) == 0) continue;
       const GroupedItem it = item_at(index);
-      const int chunks = chunks_of(it);
-      a.init(it.a, p.lda, it.K, it.rows, it.readable_rows, p.prescale_a, t);
-      b.init(it.b, p.ldb, it.K, it.cols, it.readable_cols, p.prescale_b, t);
-      for (int c = 0; c < chunks; ++c) {
-        char* stage = lds + (c & 1) * STAGE_BYTES;
-        a.fetch_any(xa[0], c), b.fetch_any(xb[0], c);
-        a.complete(xa[0], c), b.complete(xb[0], c);
-        a.deposit_with_care(xa[0], stage);
-        b.deposit_with_care(xb[0], stage + REGION_BYTES);
-        block_barrier();
-      }
-      if (chunks & 1) block_barrier();
+      auto again = [&](auto&& adapter) {
+        int number = 0;
+        adapter(number);
+        if (number & 1) block_barrier();
+        a.init(it.a, p.lda, it.K, it.rows, it.readable_rows, p.prescale_a, t);
+        b.init(it.b, p.ldb, it.K, it.cols, it.readable_cols, p.prescale_b, t);
+        const int chunks = chunks_of(it);
+        for (int c = 0; c < chunks; ++c) {
+          float xa[VALUES], xb[VALUES];
+          char* stage = lds + (c & 1) * STAGE_BYTES;
+          a.fetch_any(xa, c), b.fetch_any(xb, c);
+          a.complete(xa, c), b.complete(xb, c);
+          a.deposit_with_care(xa, stage);
+          b.deposit_with_care(xb, stage + REGION_BYTES);
+          block_barrier();
+        }
+        if (chunks & 1) block_barrier();
+      };
+      if constexpr (ADAPTERS)
+        for_adapters(it, [&](int group, int lo, int hi) { again([&](int& number) { deposit_adapter(it, group, lo, hi, number, std::true_type{}); }); });
+      again([](int&) {});
     }
     return;
   }
@@ -501,38 +604,41 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_kernel(const Group
       __builtin_amdgcn_sched_barrier(0);
     });
   };
-  // A tile's sums, main + correction, in acc_main; returns whether all of them are finite.
-  auto multiply = [&](int chunks) {
+  // A tile's sums, main + correction, in acc_main; returns whether all of them are finite.  ADAPTERS: their chunks first.
+  auto multiply = [&](int adapter_chunks, int own_chunks) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc_main[i][j][v] = 0.0f, acc_corr[i][j][v] = 0.0f;
-    if (chunks == 0) return true;
-    block_barrier();  // chunk 0 is there
-    static_for<READS>([&](auto r_c) { read_fragment(std::integral_constant<int, 0>{}, r_c, lds, lane_off[0]); });
-    auto steps_within = [&](const char* stage) {
-      static_for<K_STEPS - 1>([&](auto ks_c) {
-        constexpr int ks = decltype(ks_c)::value;
-        step(std::integral_constant<int, ks & 1>{}, stage, lane_off[ks + 1]);
-      });
-    };
-    auto chunk_and_next = [&](const char* stage, const char* next) {
-      steps_within(stage);
-      block_barrier();  // this chunk has been read to the end, the next one is there
-      step(std::integral_constant<int, (K_STEPS - 1) & 1>{}, next, lane_off[0]);
-    };
-    int left = chunks - 1;
-    for (; left >= 2; left -= 2) {
-      chunk_and_next(lds, lds + STAGE_BYTES);
-      chunk_and_next(lds + STAGE_BYTES, lds);
+    for (int part = ADAPTERS ? 0 : 1; part < 2; ++part) {
+      const int chunks = part == 0 ? adapter_chunks : own_chunks;
+      if (chunks == 0) continue;
+      block_barrier();  // chunk 0 is there
+      static_for<READS>([&](auto r_c) { read_fragment(std::integral_constant<int, 0>{}, r_c, lds, lane_off[0]); });
+      auto steps_within = [&](const char* stage) {
+        static_for<K_STEPS - 1>([&](auto ks_c) {
+          constexpr int ks = decltype(ks_c)::value;
+          step(std::integral_constant<int, ks & 1>{}, stage, lane_off[ks + 1]);
+        });
+      };
+      auto chunk_and_next = [&](const char* stage, const char* next) {
+        steps_within(stage);
+        block_barrier();  // this chunk has been read to the end, the next one is there
+        step(std::integral_constant<int, (K_STEPS - 1) & 1>{}, next, lane_off[0]);
+      };
+      int left = chunks - 1;
+      for (; left >= 2; left -= 2) {
+        chunk_and_next(lds, lds + STAGE_BYTES);
+        chunk_and_next(lds + STAGE_BYTES, lds);
+      }
+      if (left == 1) chunk_and_next(lds, lds + STAGE_BYTES);
+      const char* last = lds + ((chunks - 1) & 1) * STAGE_BYTES;
+      steps_within(last);
+      step(std::integral_constant<int, (K_STEPS - 1) & 1>{}, last, lane_off[0]);  // (what it reads is not used)
+      if (chunks & 1) block_barrier();
     }
-    if (left == 1) chunk_and_next(lds, lds + STAGE_BYTES);
-    const char* last = lds + ((chunks - 1) & 1) * STAGE_BYTES;
-    steps_within(last);
-    step(std::integral_constant<int, (K_STEPS - 1) & 1>{}, last, lane_off[0]);  // (what it reads is not used)
-    if (chunks & 1) block_barrier();
     float largest = 0.0f;
     constexpr float corr_scale = METHOD == kMethodFp16Split ? 0x1p-11f : 1.0f;
 #pragma unroll
@@ -547,7 +653,9 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_kernel(const Group
     return __builtin_amdgcn_ballot_w64(!(largest <= 3.402823466e+38f)) == 0;
   };
   // a lane owns one row per 32 x 32 block; register v of it is the matrix instruction's column 8 (v / 4) + 4 (lane / 32) + v % 4
-  auto write_tile = [&](const GroupedItem& it) {
+  // ADAPTERS: `columns` of the tile's columns, a bit each
+  auto write_tile = [&](const GroupedItem& it, const uint64_t (&columns)[2]) {
+    auto mine = [&](int c) { return c < it.cols && (!ADAPTERS || (columns[c >> 6] >> (c & 63) & 1) != 0); };
     // (the lane hidden from the optimizer: it would work out the columns' offsets before the first tile and keep them all)
     int lane_here = lane;
     asm volatile("" : "+v"(lane_here));
@@ -565,37 +673,61 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_kernel(const Group
           if (p.beta != 0.0f) {
             float c_in[16];
 #pragma unroll
-            for (int v = 0; v < 16; ++v) c_in[v] = whole || tile_column(j, v) < it.cols ? load_global(dst + tile_column(j, v) * p.ldc) : 0.0f;
+            for (int v = 0; v < 16; ++v) c_in[v] = whole || mine(tile_column(j, v)) ? load_global(dst + tile_column(j, v) * p.ldc) : 0.0f;
 #pragma unroll
             for (int v = 0; v < 16; ++v)
-              if (whole || tile_column(j, v) < it.cols)
-                store_result(dst + tile_column(j, v) * p.ldc, scaled_sum(it.alpha, acc_main[i][j][v] * p.out_scale, p.beta, c_in[v]));
+              if (whole || mine(tile_column(j, v)))
+                store_result(dst + tile_column(j, v) * p.ldc, scaled_sum(p.alpha, acc_main[i][j][v] * p.out_scale, p.beta, c_in[v]));
           } else {
 #pragma unroll
             for (int v = 0; v < 16; ++v)
-              if (whole || tile_column(j, v) < it.cols) store_result(dst + tile_column(j, v) * p.ldc, it.alpha * (acc_main[i][j][v] * p.out_scale));
+              if (whole || mine(tile_column(j, v))) store_result(dst + tile_column(j, v) * p.ldc, p.alpha * (acc_main[i][j][v] * p.out_scale));
           }
         };
-        if (it.cols == kGroupedTile) store_all(std::true_type{});
+        if (it.cols == kGroupedTile && (!ADAPTERS || (columns[0] & columns[1]) == ~0ull)) store_all(std::true_type{});
         else store_all(std::false_type{});
       }
     }
   };
-  // (one loop for both passes, so that what they do is in the program once)
+  // (one loop for both passes, so that what they do is in the program once.  In the second one, a tile with adapters is made
+  // once for each of them and once without any, and the columns concerned are written: an adapter that is not finite has
+  // nothing to do with the columns of the others)
   for (int pass = 0;; ++pass) {
     int number = 0, left_out = 0;
     for (int index = position; index < items; index += step_items, ++number) {
       if (pass == 1 && uniform(*reinterpret_cast<const int*>(not_finite[number])) == 0) continue;
       const GroupedItem it = item_at(index);
-      const bool finite = multiply(chunks_of(it));
-      bool mine = finite;
-      if (pass == 0) {
-        if (lane == 0) not_finite[number][which] = !finite;
-        left_out |= !finite;
-      } else {
-        mine = uniform((int)not_finite[number][which]) != 0;
+      const int adapters = ADAPTERS ? adapters_of(it) : 0;
+      uint64_t covered[2] = {0, 0};
+      for (int turn = 0; turn <= (ADAPTERS && pass == 1 ? adapters : 0); ++turn) {
+        uint64_t columns[2] = {~0ull, ~0ull};
+        int adapter_chunks = 0;
+        if constexpr (ADAPTERS) {
+          if (pass == 0) {
+            adapter_chunks = adapters * rank_chunks;
+          } else if (turn < adapters) {
+            adapter_chunks = rank_chunks;
+            int at = 0;
+            for_adapters(it, [&](int, int lo, int hi) {
+              if (at++ != turn) return;
+              auto below = [](int c, int word) { return c <= 64 * word ? 0ull : c >= 64 * word + 64 ? ~0ull : (1ull << (c - 64 * word)) - 1; };
+#pragma unroll
+              for (int w = 0; w < 2; ++w) columns[w] = below(hi, w) & ~below(lo, w), covered[w] |= columns[w];
+            });
+          } else {
+            columns[0] = ~covered[0], columns[1] = ~covered[1];
+          }
+        }
+        const bool finite = multiply(adapter_chunks, chunks_of(it));
+        bool write = finite;
+        if (pass == 0) {
+          if (lane == 0) not_finite[number][which] = !finite;
+          left_out |= !finite;
+        } else {
+          write = uniform((int)not_finite[number][which]) != 0;
+        }
+        if (write) write_tile(it, columns);
       }
-      if (mine) write_tile(it);
     }
     if (pass == 1) return;
     if (lane == 0) any_not_finite[which] = left_out;

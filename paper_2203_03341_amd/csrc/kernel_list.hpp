@@ -142,23 +142,31 @@ ECGEMM_WIDE_GROUP template __global__ void wide_kernel<kMethodFp16Split, true, f
 ECGEMM_WIDE_GROUP template __global__ void wide_kernel<kMethodFp16Split, true, true>(const WideParams);
 
 #define ECGEMM_GROUPED_KERNELS_OF(GROUP, METHOD, SCALED)                                                  \
-  GROUP template __global__ void grouped_kernel<METHOD, false, false, SCALED>(const GroupedParams);  \
-  GROUP template __global__ void grouped_kernel<METHOD, false, true, SCALED>(const GroupedParams);   \
-  GROUP template __global__ void grouped_kernel<METHOD, true, false, SCALED>(const GroupedParams);   \
-  GROUP template __global__ void grouped_kernel<METHOD, true, true, SCALED>(const GroupedParams);
+  GROUP template __global__ void grouped_kernel<METHOD, false, false, SCALED, false>(const GroupedParams);  \
+  GROUP template __global__ void grouped_kernel<METHOD, false, true, SCALED, false>(const GroupedParams);   \
+  GROUP template __global__ void grouped_kernel<METHOD, true, false, SCALED, false>(const GroupedParams);   \
+  GROUP template __global__ void grouped_kernel<METHOD, true, true, SCALED, false>(const GroupedParams);
 ECGEMM_GROUPED_KERNELS_OF(ECGEMM_GROUPED_FP16_GROUP, kMethodFp16Split, false)
 ECGEMM_GROUPED_KERNELS_OF(ECGEMM_GROUPED_FP16_GROUP, kMethodFp16Split, true)  // for handles with a pre-scaling
 ECGEMM_GROUPED_KERNELS_OF(ECGEMM_GROUPED_BF16_GROUP, kMethodBf16Full, false)
 ECGEMM_GROUPED_KERNELS_OF(ECGEMM_GROUPED_BF16_GROUP, kMethodBf16Full, true)
+ECGEMM_GROUPED_FP16_GROUP template __global__ void grouped_kernel<kMethodFp16Split, false, true, false, true>(const GroupedParams);
+ECGEMM_GROUPED_FP16_GROUP template __global__ void grouped_kernel<kMethodFp16Split, true, true, false, true>(const GroupedParams);
+ECGEMM_GROUPED_BF16_GROUP template __global__ void grouped_kernel<kMethodBf16Full, false, true, false, true>(const GroupedParams);
+ECGEMM_GROUPED_BF16_GROUP template __global__ void grouped_kernel<kMethodBf16Full, true, true, false, true>(const GroupedParams);
 
-ECGEMM_NARROW_GROUP template __global__ void narrow_kernel<false, false>(const NarrowParams);
-ECGEMM_NARROW_GROUP template __global__ void narrow_kernel<false, true>(const NarrowParams);
-ECGEMM_NARROW_GROUP template __global__ void narrow_kernel<true, false>(const NarrowParams);
-ECGEMM_NARROW_GROUP template __global__ void narrow_kernel<true, true>(const NarrowParams);
-ECGEMM_NARROW_GROUP template __global__ void adapter_down_kernel<false, false>(const AdapterDownParams);
-ECGEMM_NARROW_GROUP template __global__ void adapter_down_kernel<false, true>(const AdapterDownParams);
-ECGEMM_NARROW_GROUP template __global__ void adapter_down_kernel<true, false>(const AdapterDownParams);
-ECGEMM_NARROW_GROUP template __global__ void adapter_down_kernel<true, true>(const AdapterDownParams);
+ECGEMM_NARROW_GROUP template __global__ void narrow_kernel<false, false, 4>(const NarrowParams);
+ECGEMM_NARROW_GROUP template __global__ void narrow_kernel<false, true, 4>(const NarrowParams);
+ECGEMM_NARROW_GROUP template __global__ void narrow_kernel<true, false, 1>(const NarrowParams);
+ECGEMM_NARROW_GROUP template __global__ void narrow_kernel<true, true, 1>(const NarrowParams);
+ECGEMM_NARROW_GROUP template __global__ void narrow_kernel<true, false, 2>(const NarrowParams);
+ECGEMM_NARROW_GROUP template __global__ void narrow_kernel<true, true, 2>(const NarrowParams);
+ECGEMM_NARROW_GROUP template __global__ void adapter_down_kernel<false, false, 4>(const AdapterDownParams);
+ECGEMM_NARROW_GROUP template __global__ void adapter_down_kernel<false, true, 4>(const AdapterDownParams);
+ECGEMM_NARROW_GROUP template __global__ void adapter_down_kernel<true, false, 1>(const AdapterDownParams);
+ECGEMM_NARROW_GROUP template __global__ void adapter_down_kernel<true, true, 1>(const AdapterDownParams);
+ECGEMM_NARROW_GROUP template __global__ void adapter_down_kernel<true, false, 2>(const AdapterDownParams);
+ECGEMM_NARROW_GROUP template __global__ void adapter_down_kernel<true, true, 2>(const AdapterDownParams);
 ECGEMM_NARROW_GROUP template __global__ void adapter_up_kernel<false>(const AdapterUpParams);
 ECGEMM_NARROW_GROUP template __global__ void adapter_up_kernel<true>(const AdapterUpParams);
 

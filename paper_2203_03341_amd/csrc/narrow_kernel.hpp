@@ -8,8 +8,11 @@
 //   * a block takes 16 rows (64 where rows are contiguous) and all the group's columns, its eight waves share the depth
 //     between them, each taking every eighth stretch, so that the block reads runs of 2 KiB of every row; the eight sums
 //     meet in LDS and are added in order.
-//   * lane l of a wave has row and column l % 16 and takes a float4 of the depth at 4 (l / 16): element e of it is that
-//     lane's part of instruction e, for either operand, so both are read 16 bytes at a time and need no rearrangement.
+//   * an instruction takes row and column l % 16 from lane l.  Loads in that order have neighbouring lanes in different rows,
+//     and the memory path takes 16 bytes a cycle then instead of 64 (4096 x 4096 times 32 columns 27 us, three quarters of
+//     them that): where its depth is contiguous, an operand is read along it, eight lanes a row, and changes lanes in a part
+//     of LDS that is the wave's own.
+//   * lane l's float4 at 4 (l / 16) of a quad of 16 k is its part of four instructions, for either operand.
 //   * two stretches are in flight in registers while a third one is multiplied.
 #pragma once
 #include "grouped_kernel.hpp"
@@ -17,69 +20,83 @@
 namespace ecgemm {
 
 typedef float narrow_acc_t __attribute__((ext_vector_type(4)));
-constexpr int kNarrowWaves = 8, kNarrowThreads = 64 * kNarrowWaves;
-constexpr int kNarrowColumns = 32;  // of one pass over the rows
+typedef float float4_any_t __attribute__((ext_vector_type(4), aligned(4)));
+constexpr int kNarrowColumns = 32;  // of one pass over the rows; twice that in adapter_down_kernel
 
 // What one wave adds up: rows of S (FR blocks of 16) times columns of T (NF blocks of 16).  S(r, k) = s[k + r lds] (S_DEPTH) or
 // s[r + k lds]; T(c, k) alike.  Which row lane l's element v of acc[f][.] belongs to: row_of.
 template <bool S_DEPTH, bool T_DEPTH, int FR, int NF>
 struct WaveProduct {
   static_assert(S_DEPTH || FR == 4, "rows contiguous: four rows a load");
-  static constexpr int STRETCH = S_DEPTH && FR == 1 ? (T_DEPTH && NF == 1 ? 64 : 32) : 16;  // of the depth per step
+  static_assert(NF == 1 || NF == 2 || NF == 4, "columns contiguous: one load");
+  static constexpr int STRETCH = S_DEPTH && FR <= 2 ? 32 : 16;  // of the depth per step
   static constexpr int QUADS = STRETCH / 16;
+  // the wave's part of LDS: 16 FR rows of S and 16 NF columns of T, whichever of them have their depth contiguous, PITCH apart
+  static constexpr int LANES = STRETCH / 4, AT_ONCE = 64 / LANES, PITCH = STRETCH + 4;  // lanes per row, rows per load
+  static constexpr int S_LOADS = FR * 16 / AT_ONCE, T_LOADS = NF * 16 / AT_ONCE;
+  static constexpr int SPACE = (S_DEPTH ? 16 * FR * PITCH : 0) + (T_DEPTH ? 16 * NF * PITCH : 0);  // floats
+
   const float* s;
   const float* t;
   int64_t lds, ldt, K;
   int rows, cols;  // that exist, at least 1
   int lane;
+  float* space;
   struct Values {
-    float s[FR][QUADS][4], t[NF][QUADS][4];  // S_DEPTH: [row block][..][e]; else [u][..][e] of rows 4 (l % 16) + u
+    float s[S_DEPTH ? S_LOADS : FR][S_DEPTH ? 1 : QUADS][4];  // S_DEPTH: as loaded; else [u][quad][e] of rows 4 (l % 16) + u
+    float t[T_DEPTH ? T_LOADS : NF][T_DEPTH ? 1 : QUADS][4];
   };
 
   __device__ __forceinline__ static int row_of(int f, int v, int lane) { return S_DEPTH ? 16 * f + 4 * (lane >> 4) + v : 16 * (lane >> 4) + 4 * v + f; }
+  // which column lane l's part of acc[.][n] belongs to: where columns are contiguous, a load takes NF of them
+  __device__ __forceinline__ static int column_of(int n, int lane) { return T_DEPTH ? 16 * n + (lane & 15) : NF * (lane & 15) + n; }
+  __device__ __forceinline__ int loaded_row(int j) const { return AT_ONCE * j + lane / LANES; }
+  __device__ __forceinline__ static int clamped(int i, int count) { return i < count ? i : count - 1; }
 
-  __device__ __forceinline__ int64_t k_of(int64_t k0, int q) const { return k0 + 16 * q + 4 * (lane >> 4); }
-  __device__ __forceinline__ int row(int f) const {
-    const int r = S_DEPTH ? 16 * f + (lane & 15) : 4 * (lane & 15) + f;
-    return r < rows ? r : rows - 1;
-  }
-  __device__ __forceinline__ int column(int n) const {
-    const int c = 16 * n + (lane & 15);
-    return c < cols ? c : cols - 1;
-  }
   // the stretch from k0 on (the same for the wave), which lies inside the depth; rows contiguous: all 64 rows exist.  Buffer
   // loads: a scalar base, an offset per lane that never changes, and a scalar offset per load.
   __device__ __forceinline__ void fetch(Values& x, int64_t k0) const {
     const auto from_s = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(s + (S_DEPTH ? k0 : k0 * lds)), 0, -1, 0x00020000);
     const auto from_t = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(t + (T_DEPTH ? k0 : k0 * ldt)), 0, -1, 0x00020000);
-    const int s_step = (int)(4 * lds), t_step = (int)(4 * ldt), quad = 4 * (lane >> 4);
+    const int s_step = (int)(4 * lds), t_step = (int)(4 * ldt), quad = 4 * (lane >> 4), k_here = 4 * (lane % LANES);
+    if constexpr (S_DEPTH) {
 #pragma unroll
-    for (int q = 0; q < QUADS; ++q) {
-      if constexpr (S_DEPTH) {
+      for (int j = 0; j < S_LOADS; ++j) {
+        const source4_t v = __builtin_bit_cast(source4_t, __builtin_amdgcn_raw_buffer_load_b128(from_s, (int)((clamped(loaded_row(j), rows) * lds + k_here) * 4), 0, 0));
 #pragma unroll
-        for (int f = 0; f < FR; ++f) {
-          const source4_t v = __builtin_bit_cast(source4_t, __builtin_amdgcn_raw_buffer_load_b128(from_s, (int)((row(f) * lds + quad) * 4) + 64 * q, 0, 0));
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x.s[f][q][e] = v[e];
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const source4_t v = __builtin_bit_cast(source4_t, __builtin_amdgcn_raw_buffer_load_b128(from_s, (int)((4 * (lane & 15) + quad * lds) * 4), (16 * q + e) * s_step, 0));
-#pragma unroll
-          for (int f = 0; f < FR; ++f) x.s[f][q][e] = v[f];
-        }
+        for (int e = 0; e < 4; ++e) x.s[j][0][e] = v[e];
       }
+    } else {
 #pragma unroll
-      for (int n = 0; n < NF; ++n) {
-        if constexpr (T_DEPTH) {
-          const source4_t v = __builtin_bit_cast(source4_t, __builtin_amdgcn_raw_buffer_load_b128(from_t, (int)((column(n) * ldt + quad) * 4) + 64 * q, 0, 0));
+      for (int i = 0; i < 4 * QUADS; ++i) {
+        const source4_t v = __builtin_bit_cast(source4_t, __builtin_amdgcn_raw_buffer_load_b128(from_s, (int)((4 * (lane & 15) + quad * lds) * 4), (16 * (i / 4) + i % 4) * s_step, 0));
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x.t[n][q][e] = v[e];
+        for (int f = 0; f < FR; ++f) x.s[f][i / 4][i % 4] = v[f];
+      }
+    }
+    if constexpr (T_DEPTH) {
+#pragma unroll
+      for (int j = 0; j < T_LOADS; ++j) {
+        const source4_t v = __builtin_bit_cast(source4_t, __builtin_amdgcn_raw_buffer_load_b128(from_t, (int)((clamped(loaded_row(j), cols) * ldt + k_here) * 4), 0, 0));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x.t[j][0][e] = v[e];
+      }
+    } else {
+      // (the last lanes' columns do not exist where cols < 16 NF: they read the last ones that do)
+      const int first = NF * (lane & 15), at = (int)(((first < cols ? first : cols - NF) + quad * ldt) * 4);
+#pragma unroll
+      for (int i = 0; i < 4 * QUADS; ++i) {
+        const int by = (16 * (i / 4) + i % 4) * t_step;
+        if constexpr (NF == 1) {
+          x.t[0][i / 4][i % 4] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(from_t, at, by, 0));
+        } else if constexpr (NF == 2) {
+          typedef float float2_t __attribute__((ext_vector_type(2)));
+          const float2_t v = __builtin_bit_cast(float2_t, __builtin_amdgcn_raw_buffer_load_b64(from_t, at, by, 0));
+          x.t[0][i / 4][i % 4] = v[0], x.t[1][i / 4][i % 4] = v[1];
         } else {
+          const source4_t v = __builtin_bit_cast(source4_t, __builtin_amdgcn_raw_buffer_load_b128(from_t, at, by, 0));
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            x.t[n][q][e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(from_t, (int)((column(n) + quad * ldt) * 4), (16 * q + e) * t_step, 0));
+          for (int f = 0; f < 4; ++f) x.t[f][i / 4][i % 4] = v[f];
         }
       }
     }
@@ -87,40 +104,83 @@ struct WaveProduct {
   // any stretch, value by value: zero behind the depth
   __device__ __forceinline__ void fetch_any(Values& x, int64_t k0) const {
 #pragma unroll
-    for (int q = 0; q < QUADS; ++q)
+    for (int i = 0; i < (S_DEPTH ? S_LOADS : FR * QUADS); ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int64_t k = k_of(k0, q) + e;
-        const bool inside = k < K;
+        const int64_t k = k0 + e + (S_DEPTH ? 4 * (lane % LANES) : 16 * (i % QUADS) + 4 * (lane >> 4));
+        const int r = clamped(S_DEPTH ? loaded_row(i) : 4 * (lane & 15) + i / QUADS, rows);
+        x.s[S_DEPTH ? i : i / QUADS][S_DEPTH ? 0 : i % QUADS][e] = k < K ? s[S_DEPTH ? r * lds + k : r + k * lds] : 0.0f;
+      }
 #pragma unroll
-        for (int f = 0; f < FR; ++f) x.s[f][q][e] = inside ? s[S_DEPTH ? row(f) * lds + k : row(f) + k * lds] : 0.0f;
+    for (int i = 0; i < (T_DEPTH ? T_LOADS : NF * QUADS); ++i)
 #pragma unroll
-        for (int n = 0; n < NF; ++n) x.t[n][q][e] = inside ? t[T_DEPTH ? column(n) * ldt + k : column(n) + k * ldt] : 0.0f;
+      for (int e = 0; e < 4; ++e) {
+        const int64_t k = k0 + e + (T_DEPTH ? 4 * (lane % LANES) : 16 * (i % QUADS) + 4 * (lane >> 4));
+        const int c = clamped(T_DEPTH ? loaded_row(i) : column_of(i / QUADS, lane), cols);
+        x.t[T_DEPTH ? i : i / QUADS][T_DEPTH ? 0 : i % QUADS][e] = k < K ? t[T_DEPTH ? c * ldt + k : c + k * ldt] : 0.0f;
       }
   }
-  __device__ __forceinline__ static void multiply(const Values& x, narrow_acc_t (&acc)[FR][NF]) {
+  __device__ __forceinline__ void multiply(const Values& x, narrow_acc_t (&acc)[FR][NF]) const {
+    float* const s_space = space;
+    float* const t_space = space + (S_DEPTH ? 16 * FR * PITCH : 0);
+    // (a wave's LDS instructions are carried out in order: nothing but the compiler has to be kept from changing it)
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+    if constexpr (S_DEPTH)
 #pragma unroll
-    for (int q = 0; q < QUADS; ++q)
+      for (int j = 0; j < S_LOADS; ++j) *reinterpret_cast<narrow_acc_t*>(s_space + loaded_row(j) * PITCH + 4 * (lane % LANES)) = narrow_acc_t{x.s[j][0][0], x.s[j][0][1], x.s[j][0][2], x.s[j][0][3]};
+    if constexpr (T_DEPTH)
+#pragma unroll
+      for (int j = 0; j < T_LOADS; ++j) *reinterpret_cast<narrow_acc_t*>(t_space + loaded_row(j) * PITCH + 4 * (lane % LANES)) = narrow_acc_t{x.t[j][0][0], x.t[j][0][1], x.t[j][0][2], x.t[j][0][3]};
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int q = 0; q < QUADS; ++q) {
+      narrow_acc_t from_s[FR], from_t[NF];
+#pragma unroll
+      for (int f = 0; f < FR; ++f) {
+        if constexpr (S_DEPTH) from_s[f] = *reinterpret_cast<const narrow_acc_t*>(s_space + (16 * f + (lane & 15)) * PITCH + 16 * q + 4 * (lane >> 4));
+        else from_s[f] = narrow_acc_t{x.s[f][q][0], x.s[f][q][1], x.s[f][q][2], x.s[f][q][3]};
+      }
+#pragma unroll
+      for (int n = 0; n < NF; ++n) {
+        if constexpr (T_DEPTH) from_t[n] = *reinterpret_cast<const narrow_acc_t*>(t_space + (16 * n + (lane & 15)) * PITCH + 16 * q + 4 * (lane >> 4));
+        else from_t[n] = narrow_acc_t{x.t[n][q][0], x.t[n][q][1], x.t[n][q][2], x.t[n][q][3]};
+      }
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
         for (int f = 0; f < FR; ++f)
 #pragma unroll
-          for (int n = 0; n < NF; ++n) acc[f][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(x.s[f][q][e], x.t[n][q][e], acc[f][n], 0, 0, 0);
+          for (int n = 0; n < NF; ++n) acc[f][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(from_s[f][e], from_t[n][e], acc[f][n], 0, 0, 0);
+    }
   }
-  // adds stretches first, first + step, ... to acc (all in units of STRETCH)
-  __device__ __forceinline__ void run(narrow_acc_t (&acc)[FR][NF], int64_t first, int64_t step) const {
-    const int64_t whole = S_DEPTH || rows >= 64 ? K / STRETCH : 0, all = (K + STRETCH - 1) / STRETCH;
+  // Adds stretches first, first + step, ... to acc (all in units of STRETCH).  `turn` of 2^32 of the way through the depth is
+  // where it begins, going on from the front when it comes to the end: blocks that start together would otherwise all read
+  // the same columns of rows that lie a power of two apart, from a few of the memory's channels.
+  __device__ __forceinline__ void run(narrow_acc_t (&acc)[FR][NF], int64_t first, int64_t step, unsigned turn) const {
+    const bool vectors = (S_DEPTH || rows >= 64) && (T_DEPTH || cols % NF == 0);
+    const int64_t whole = vectors ? K / STRETCH : 0, all = (K + STRETCH - 1) / STRETCH;
+    const int64_t begin = (int64_t)(((uint64_t)turn * (uint64_t)whole) >> 32);
+    auto k_at = [&](int64_t stretch) {
+      const int64_t turned = stretch + begin;
+      return (turned < whole ? turned : turned - whole) * STRETCH;
+    };
     int64_t i = first;
     if (i < whole) {
       Values x[2];
-      fetch(x[0], i * STRETCH);
-      if (i + step < whole) fetch(x[1], (i + step) * STRETCH);
+      fetch(x[0], k_at(i));
+      if (i + step < whole) fetch(x[1], k_at(i + step));
       for (; i + 3 * step < whole; i += 2 * step) {
+        // (kept in this order: a product drawn in front of the loads behind it would wait for all that is in flight)
         multiply(x[0], acc);
-        fetch(x[0], (i + 2 * step) * STRETCH);
+        __builtin_amdgcn_sched_barrier(0);
+        fetch(x[0], k_at(i + 2 * step));
+        __builtin_amdgcn_sched_barrier(0);
         multiply(x[1], acc);
-        fetch(x[1], (i + 3 * step) * STRETCH);
+        __builtin_amdgcn_sched_barrier(0);
+        fetch(x[1], k_at(i + 3 * step));
+        __builtin_amdgcn_sched_barrier(0);
       }
       multiply(x[0], acc);
       i += step;
@@ -129,7 +189,7 @@ struct WaveProduct {
         i += step;
       }
       if (i < whole) {
-        fetch(x[0], i * STRETCH);
+        fetch(x[0], k_at(i));
         multiply(x[0], acc);
         i += step;
       }
@@ -143,16 +203,15 @@ struct WaveProduct {
 };
 
 // The block's sums over the whole depth, in `sums`[column][row] (ROWS + 1 apart): all waves' partial sums in order.
-template <bool S_DEPTH>
-constexpr int narrow_rows() { return S_DEPTH ? 16 : 64; }
-template <bool S_DEPTH>
-struct NarrowSums {
-  float of_wave[kNarrowWaves][kNarrowColumns][narrow_rows<S_DEPTH>() + 1];
+constexpr int kNarrowWaves = 8, kNarrowThreads = 64 * kNarrowWaves;
+template <bool S_DEPTH, bool T_DEPTH, int FR, bool WIDE>
+union NarrowSums {
+  float space[kNarrowWaves][WaveProduct<S_DEPTH, T_DEPTH, FR, WIDE ? 4 : 2>::SPACE + 4];  // while the waves multiply
+  float of_wave[kNarrowWaves][WIDE ? 2 * kNarrowColumns : kNarrowColumns][16 * FR + 1];
 };
-template <bool S_DEPTH, bool T_DEPTH, int NF>
+template <bool S_DEPTH, bool T_DEPTH, int FR, int NF, bool WIDE>
 __device__ __forceinline__ void narrow_pass(const float* s, int64_t lds, int rows, const float* t, int64_t ldt, int cols, int64_t K,
-                                            NarrowSums<S_DEPTH>& sums) {
-  constexpr int FR = S_DEPTH ? 1 : 4;
+                                            NarrowSums<S_DEPTH, T_DEPTH, FR, WIDE>& sums) {
   typedef WaveProduct<S_DEPTH, T_DEPTH, FR, NF> Product;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   narrow_acc_t acc[FR][NF];
@@ -160,26 +219,28 @@ __device__ __forceinline__ void narrow_pass(const float* s, int64_t lds, int row
   for (int f = 0; f < FR; ++f)
 #pragma unroll
     for (int n = 0; n < NF; ++n) acc[f][n] = narrow_acc_t{0.0f, 0.0f, 0.0f, 0.0f};
-  const Product product{s, t, lds, ldt, K, rows, cols, lane};
-  product.run(acc, wave, kNarrowWaves);
+  const Product product{s, t, lds, ldt, K, rows, cols, lane, sums.space[wave]};
+  product.run(acc, wave, kNarrowWaves, blockIdx.x * 0x9E3779B1u);
+  __syncthreads();  // every wave is through with its space
 #pragma unroll
   for (int f = 0; f < FR; ++f)
 #pragma unroll
     for (int n = 0; n < NF; ++n)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) sums.of_wave[wave][16 * n + (lane & 15)][Product::row_of(f, v, lane)] = acc[f][n][v];
+      for (int v = 0; v < 4; ++v) sums.of_wave[wave][Product::column_of(n, lane)][Product::row_of(f, v, lane)] = acc[f][n][v];
 }
 // ends with a barrier; element (row, column) is then narrow_sum(...)
-template <bool S_DEPTH, bool T_DEPTH>
+template <bool S_DEPTH, bool T_DEPTH, int FR, bool WIDE>
 __device__ __forceinline__ void narrow_block(const float* s, int64_t lds, int rows, const float* t, int64_t ldt, int cols, int64_t K,
-                                             NarrowSums<S_DEPTH>& sums) {
+                                             NarrowSums<S_DEPTH, T_DEPTH, FR, WIDE>& sums) {
   __syncthreads();  // the sums of the pass before have been read
-  if (cols > 16) narrow_pass<S_DEPTH, T_DEPTH, 2>(s, lds, rows, t, ldt, cols, K, sums);
-  else narrow_pass<S_DEPTH, T_DEPTH, 1>(s, lds, rows, t, ldt, cols, K, sums);
+  if (WIDE && cols > 32) narrow_pass<S_DEPTH, T_DEPTH, FR, WIDE ? 4 : 2, WIDE>(s, lds, rows, t, ldt, cols, K, sums);
+  else if (cols > 16) narrow_pass<S_DEPTH, T_DEPTH, FR, 2, WIDE>(s, lds, rows, t, ldt, cols, K, sums);
+  else narrow_pass<S_DEPTH, T_DEPTH, FR, 1, WIDE>(s, lds, rows, t, ldt, cols, K, sums);
   __syncthreads();
 }
-template <bool S_DEPTH>
-__device__ __forceinline__ float narrow_sum(const NarrowSums<S_DEPTH>& sums, int row, int column) {
+template <bool S_DEPTH, bool T_DEPTH, int FR, bool WIDE>
+__device__ __forceinline__ float narrow_sum(const NarrowSums<S_DEPTH, T_DEPTH, FR, WIDE>& sums, int row, int column) {
   float c = 0.0f;
 #pragma unroll
   for (int w = 0; w < kNarrowWaves; ++w) c += sums.of_wave[w][column][row];
@@ -216,8 +277,8 @@ __device__ __forceinline__ void find_adapters(const int64_t* offsets, int64_t gr
   __syncthreads();
   for (int64_t g = threadIdx.x; g < groups; g += threads) {
     const int64_t begin = clamp_offset(offsets[g], 0, N), end = clamp_offset(offsets[g + 1], begin, N);
+    const int a = index[g];
     if (begin < first + count && end > first && begin < end) {
-      const int a = index[g];
       if (a >= 0 && a < matrices)
         for (int64_t j = begin > first ? begin : first; j < end && j < first + count; ++j) adapter[j - first] = a;
     }
@@ -227,10 +288,10 @@ __device__ __forceinline__ void find_adapters(const int64_t* offsets, int64_t gr
 
 // C(:, j) = alpha op(A_g) op(B)(:, j) + beta C(:, j) for the columns j of group g, at best a handful of them.  Block b: group
 // b / row_blocks, rows narrow_rows (b % row_blocks) and on.
-template <bool DEPTH_A, bool DEPTH_B>
-__global__ void __launch_bounds__(kNarrowThreads, DEPTH_A && DEPTH_B ? 4 : 2) narrow_kernel(const NarrowParams p) {
-  constexpr int ROWS = narrow_rows<DEPTH_A>();
-  __shared__ NarrowSums<DEPTH_A> sums;
+template <bool DEPTH_A, bool DEPTH_B, int FR>
+__global__ void __launch_bounds__(kNarrowThreads, DEPTH_A && FR == 1 ? 4 : 2) narrow_kernel(const NarrowParams p) {
+  constexpr int ROWS = 16 * FR;
+  __shared__ __attribute__((aligned(16))) NarrowSums<DEPTH_A, DEPTH_B, FR, false> sums;
   __shared__ int adapter[kNarrowColumns];
   const int64_t group = blockIdx.x / (unsigned)p.row_blocks;
   const int64_t m0 = (int64_t)(blockIdx.x % (unsigned)p.row_blocks) * ROWS;
@@ -257,18 +318,27 @@ __global__ void __launch_bounds__(kNarrowThreads, DEPTH_A && DEPTH_B ? 4 : 2) na
   for (int64_t n0 = begin; n0 < end; n0 += kNarrowColumns) {
     const int cols = (int)(end - n0 < kNarrowColumns ? end - n0 : kNarrowColumns);
     if (p.U != nullptr) find_adapters(p.adapter_offsets, p.adapter_groups, p.index, p.matrices, p.N, n0, cols, adapter, kNarrowThreads);
-    narrow_block<DEPTH_A, DEPTH_B>(a, p.lda, rows, p.B + (DEPTH_B ? n0 * p.ldb : n0), p.ldb, cols, matrix >= 0 ? p.K : 0, sums);
+    narrow_block<DEPTH_A, DEPTH_B, FR, false>(a, p.lda, rows, p.B + (DEPTH_B ? n0 * p.ldb : n0), p.ldb, cols, matrix >= 0 ? p.K : 0, sums);
     for (int i = threadIdx.x; i < ROWS * cols; i += kNarrowThreads) {
       const int r = i % ROWS, c = i / ROWS;
       if (r >= rows) continue;
-      float value = p.alpha * narrow_sum<DEPTH_A>(sums, r, c);
+      float value = p.alpha * narrow_sum(sums, r, c);
       if (p.U != nullptr && adapter[c] >= 0) {
         const float* u = p.U + adapter[c] * p.stride_u + (p.u_depth ? (m0 + r) * p.ldu : m0 + r);
         const float* h = p.H + (n0 + c) * p.ldh;
         const int64_t u_step = p.u_depth ? 1 : p.ldu;
         float added = 0.0f;
+        int64_t q = 0;
+        if (p.u_depth) {
+#pragma unroll 4
+          for (; q + 4 <= p.rank; q += 4) {
+            const float4_any_t u4 = *reinterpret_cast<const float4_any_t*>(u + q), h4 = *reinterpret_cast<const float4_any_t*>(h + q);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) added = __builtin_fmaf(u4[e], h4[e], added);
+          }
+        }
 #pragma unroll 8
-        for (int64_t q = 0; q < p.rank; ++q) added = __builtin_fmaf(u[q * u_step], h[q], added);
+        for (; q < p.rank; ++q) added = __builtin_fmaf(u[q * u_step], h[q], added);
         value = __builtin_fmaf(p.scales != nullptr ? p.scales[adapter[c]] : 1.0f, added, value);
       }
       float* dst = p.C + m0 + r + (n0 + c) * p.ldc;
@@ -279,7 +349,8 @@ __global__ void __launch_bounds__(kNarrowThreads, DEPTH_A && DEPTH_B ? 4 : 2) na
 
 // The first half of the adapters for many columns: H = op(D_a) op(B), the other way round: the columns of B, read once, are
 // the rows of the product, and the rank its columns.  A block takes 16 columns of B (64 where they are contiguous) whichever
-// groups they belong to, one pass for each adapter among them, and writes zero where there is none.
+// groups they belong to, one pass for each adapter among them, and writes zero where there is none.  The passes are dealt to
+// gridDim.y blocks: with one, the blocks where two requests meet take twice the time of the others.
 struct AdapterDownParams {
   const float* B;
   const float* D;
@@ -291,30 +362,33 @@ struct AdapterDownParams {
   float* H;
   int64_t ldh;
 };
-template <bool DEPTH_B, bool DEPTH_D>
-__global__ void __launch_bounds__(kNarrowThreads, DEPTH_B && DEPTH_D ? 4 : 2) adapter_down_kernel(const AdapterDownParams p) {
-  constexpr int ROWS = narrow_rows<DEPTH_B>();
-  __shared__ NarrowSums<DEPTH_B> sums;
+template <bool DEPTH_B, bool DEPTH_D, int FR>
+__global__ void __launch_bounds__(kNarrowThreads, 2) adapter_down_kernel(const AdapterDownParams p) {
+  constexpr int ROWS = 16 * FR;
+  __shared__ __attribute__((aligned(16))) NarrowSums<DEPTH_B, DEPTH_D, FR, DEPTH_B> sums;
   __shared__ int adapter[2][kNarrowColumns];
-  const int64_t j0 = (int64_t)blockIdx.x * ROWS;
+  const int64_t j0 = (int64_t)xcd_run_position(blockIdx.x, gridDim.x) * ROWS;  // (an adapter is read by few of the L2s)
   const int rows = (int)(p.N - j0 < ROWS ? p.N - j0 : ROWS);
   for (int half = 0; half < (ROWS + kNarrowColumns - 1) / kNarrowColumns; ++half)
     find_adapters(p.offsets, p.groups, p.index, p.matrices, p.N, j0 + half * kNarrowColumns, kNarrowColumns, adapter[half], kNarrowThreads);
   auto adapter_of = [&](int r) { return adapter[r / kNarrowColumns][r % kNarrowColumns]; };
-  for (int i = threadIdx.x; i < rows * (int)p.rank; i += kNarrowThreads)
-    if (adapter_of(i / (int)p.rank) < 0) p.H[i % (int)p.rank + (j0 + i / (int)p.rank) * p.ldh] = 0.0f;
+  if (blockIdx.y == 0)
+    for (int i = threadIdx.x; i < rows * (int)p.rank; i += kNarrowThreads)
+      if (adapter_of(i / (int)p.rank) < 0) p.H[i % (int)p.rank + (j0 + i / (int)p.rank) * p.ldh] = 0.0f;
+  unsigned run = 0;
   for (int first = 0; first < rows;) {
     const int a = uniform(adapter_of(first));
     int last = first + 1;  // a run of columns with the same adapter
     while (last < rows && uniform(adapter_of(last)) == a) ++last;
-    if (a >= 0) {
+    if (a >= 0 && run++ % gridDim.y == blockIdx.y) {
       const float* s = p.B + (DEPTH_B ? (j0 + first) * p.ldb : j0 + first);
-      for (int64_t q0 = 0; q0 < p.rank; q0 += kNarrowColumns) {
-        const int cols = (int)(p.rank - q0 < kNarrowColumns ? p.rank - q0 : kNarrowColumns);
-        narrow_block<DEPTH_B, DEPTH_D>(s, p.ldb, last - first, p.D + a * p.stride_d + (DEPTH_D ? q0 * p.ldd : q0), p.ldd, cols, p.K, sums);
+      constexpr int AT_ONCE = DEPTH_B ? 2 * kNarrowColumns : kNarrowColumns;
+      for (int64_t q0 = 0; q0 < p.rank; q0 += AT_ONCE) {
+        const int cols = (int)(p.rank - q0 < AT_ONCE ? p.rank - q0 : AT_ONCE);
+        narrow_block<DEPTH_B, DEPTH_D, FR, DEPTH_B>(s, p.ldb, last - first, p.D + a * p.stride_d + (DEPTH_D ? q0 * p.ldd : q0), p.ldd, cols, p.K, sums);
         for (int i = threadIdx.x; i < (last - first) * cols; i += kNarrowThreads) {
           const int c = i % cols, r = i / cols;
-          p.H[q0 + c + (j0 + first + r) * p.ldh] = narrow_sum<DEPTH_B>(sums, r, c);
+          p.H[q0 + c + (j0 + first + r) * p.ldh] = narrow_sum(sums, r, c);
         }
       }
     }
@@ -322,8 +396,9 @@ __global__ void __launch_bounds__(kNarrowThreads, DEPTH_B && DEPTH_D ? 4 : 2) ad
   }
 }
 
+constexpr int kAdapterUpColumns = 64;
 // The second half: C = scales[a] op(U_a) H + beta C in every column, before the projection is added.  A block takes 256 rows
-// of C and 32 columns, a wave 64 rows; the depth is the rank.  Bound by writing C (and by reading it, unless beta is zero).
+// of C and 64 columns, a wave 64 rows, run by run of columns with the same adapter; the depth is the rank.  Bound by writing C (and by reading it, unless beta is zero).
 struct AdapterUpParams {
   const float* U;
   const float* H;
@@ -339,57 +414,62 @@ struct AdapterUpParams {
 };
 template <bool DEPTH_U>
 __global__ void __launch_bounds__(256) adapter_up_kernel(const AdapterUpParams p) {
-  __shared__ int adapter[kNarrowColumns];
+  __shared__ int adapter[kAdapterUpColumns / kNarrowColumns][kNarrowColumns];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t n0 = (int64_t)(blockIdx.x / (unsigned)p.row_blocks) * kNarrowColumns;
+  const int64_t n0 = (int64_t)(blockIdx.x / (unsigned)p.row_blocks) * kAdapterUpColumns;
   const int64_t m0 = (int64_t)(blockIdx.x % (unsigned)p.row_blocks) * 256 + 64 * wave;
-  const int cols = (int)(p.N - n0 < kNarrowColumns ? p.N - n0 : kNarrowColumns);
-  find_adapters(p.offsets, p.groups, p.index, p.matrices, p.N, n0, cols, adapter, 256);
+  const int cols = (int)(p.N - n0 < kAdapterUpColumns ? p.N - n0 : kAdapterUpColumns);
+  for (int i = 0; i < kAdapterUpColumns / kNarrowColumns; ++i)
+    find_adapters(p.offsets, p.groups, p.index, p.matrices, p.N, n0 + i * kNarrowColumns, kNarrowColumns, adapter[i], 256);
   if (m0 >= p.M) return;
   const int rows = (int)(p.M - m0 < 64 ? p.M - m0 : 64);
-  typedef WaveProduct<DEPTH_U, true, 4, 2> Product;
-  narrow_acc_t result[4][2];
-#pragma unroll
-  for (int f = 0; f < 4; ++f)
-#pragma unroll
-    for (int n = 0; n < 2; ++n) result[f][n] = narrow_acc_t{0.0f, 0.0f, 0.0f, 0.0f};
+  auto adapter_of = [&](int c) { return uniform(adapter[c / kNarrowColumns][c % kNarrowColumns]); };
+  constexpr int NF = kAdapterUpColumns / 16;
+  typedef WaveProduct<DEPTH_U, true, 4, NF> Product;
+  __shared__ __attribute__((aligned(16))) float space[4][Product::SPACE];
   for (int first = 0; first < cols;) {
-    const int a = uniform(adapter[first]);
-    int last = first + 1;
-    while (last < cols && uniform(adapter[last]) == a) ++last;
-    if (a >= 0) {
-      narrow_acc_t acc[4][2];
-#pragma unroll
-      for (int f = 0; f < 4; ++f)
-#pragma unroll
-        for (int n = 0; n < 2; ++n) acc[f][n] = narrow_acc_t{0.0f, 0.0f, 0.0f, 0.0f};
-      const Product product{p.U + a * p.stride_u + (DEPTH_U ? m0 * p.ldu : m0), p.H + n0 * p.ldh, p.ldu, p.ldh, p.rank, rows, cols, lane};
-      product.run(acc, 0, 1);
-      const float scale = p.scales != nullptr ? p.scales[a] : 1.0f;
-      // (a column takes the sums of its own adapter; what the others made of it is not looked at)
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        const int c = 16 * n + (lane & 15);
-#pragma unroll
-        for (int f = 0; f < 4; ++f)
-#pragma unroll
-          for (int v = 0; v < 4; ++v) result[f][n][v] = c >= first && c < last ? scale * acc[f][n][v] : result[f][n][v];
-      }
-    }
-    first = last;
-  }
-#pragma unroll
-  for (int n = 0; n < 2; ++n) {
-    const int c = 16 * n + (lane & 15);
-    if (c >= cols) continue;
-    float* dst = p.C + m0 + (n0 + c) * p.ldc;
+    const int a = adapter_of(first);
+    int last = first + 1;  // a run of columns with the same adapter
+    while (last < cols && adapter_of(last) == a) ++last;
+    narrow_acc_t acc[4][NF];
 #pragma unroll
     for (int f = 0; f < 4; ++f)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const int r = Product::row_of(f, v, lane);
-        if (r < rows) dst[r] = p.beta != 0.0f ? __builtin_fmaf(p.beta, dst[r], result[f][n][v]) : result[f][n][v];
+      for (int n = 0; n < NF; ++n) acc[f][n] = narrow_acc_t{0.0f, 0.0f, 0.0f, 0.0f};
+    float scale = 0.0f;
+    if (a >= 0) {
+      const Product product{p.U + a * p.stride_u + (DEPTH_U ? m0 * p.ldu : m0), p.H + (n0 + first) * p.ldh, p.ldu, p.ldh, p.rank, rows, last - first, lane, space[wave]};
+      product.run(acc, 0, 1, 0);
+      scale = p.scales != nullptr ? p.scales[a] : 1.0f;
+    }
+#pragma unroll
+    for (int n = 0; n < NF; ++n) {
+      const int c = 16 * n + (lane & 15);
+      if (first + c >= last) continue;
+      float* dst = p.C + m0 + (n0 + first + c) * p.ldc;
+      // four rows next to each other: elements v of one block, or (rows of U contiguous) element v of four
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float4_any_t value;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) value[u] = scale * (DEPTH_U ? acc[i][n][u] : acc[u][n][i]);
+        const int r = DEPTH_U ? Product::row_of(i, 0, lane) : Product::row_of(0, i, lane);
+        if (rows == 64) {
+          float4_any_t* at = reinterpret_cast<float4_any_t*>(dst + r);
+          if (p.beta != 0.0f) {
+            const float4_any_t before = *at;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) value[u] = __builtin_fmaf(p.beta, before[u], value[u]);
+          }
+          *at = value;
+        } else {
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            if (r + u < rows) dst[r + u] = p.beta != 0.0f ? __builtin_fmaf(p.beta, dst[r + u], value[u]) : value[u];
+        }
       }
+    }
+    first = last;
   }
 }
 

@@ -529,14 +529,26 @@ def test_a_layer_of_experts_forward_and_backward(handle):
         # sqrt(depth) times the result's for independent values, and errors of independent elements add up as their root
         # does: 2 sqrt(160) 6.4e-6 / sqrt(160)
         assert off < 1.3e-5, off
-    # one difference along a random direction, in 64 bits: <grad, d> against (f(v + d) - f(v - d)) / 2; relu's corners are not met
-    # by steps this small but for a few of the 36800 values
+    # One difference along a random direction, in 64 bits: <grad, d> against (f(v + d) - f(v - d)) / 2.  f is linear in each leaf
+    # between relu's corners.  A value h that passes its corner between h - e and h + e adds e relu' on one side only, so the
+    # difference misses its part of <grad, d> by at most |df/da| |e|, added up over those that do.
+    # <grad, d> itself is off by what the gradient is, at most 1.3e-5 of its 2-norm as above, times d's: an independent random
+    # direction meets it with 1 / sqrt(count) of that, for which ten standard deviations are allowed.
+    directions = torch.Generator().manual_seed(14)
     for i, got in ((0, gx), (1, gW1), (2, gW2)):
         v = [l.detach() for l in leaves]
-        d = 1e-7 * torch.randn(v[i].shape, dtype=torch.float64)
-        f = lambda sign: (layer(*[u + sign * d if k == i else u for k, u in enumerate(v)]) * gy.cpu().double()).sum()  # noqa: E731
-        difference, along = float(f(1.0) - f(-1.0)) / 2, float((got.cpu().double() * d).sum())
-        assert abs(difference - along) <= 1e-3 * float(got.double().norm()) * float(d.norm()) / d.numel() ** 0.5 + 1e-9
+        d = 1e-7 * torch.randn(v[i].shape, generator=directions, dtype=torch.float64)
+        moved = {sign: [u + sign * d if k == i else u for k, u in enumerate(v)] for sign in (1.0, -1.0)}
+        f = {sign: (layer(*moved[sign]) * gy.cpu().double()).sum() for sign in moved}
+        difference, along = float(f[1.0] - f[-1.0]) / 2, float((got.cpu().double() * d).sum())
+        corners, at = 0.0, 0
+        for e, n in enumerate(sizes):
+            h_up, h_down = (moved[sign][0][at:at + n] @ moved[sign][1][e].t() for sign in (1.0, -1.0))
+            passing = (h_up > 0) != (h_down > 0)
+            corners += float(((gy[at:at + n].cpu().double() @ moved[1.0][2][e]).abs() * (h_up - h_down).abs() / 2)[passing].sum())
+            at += n
+        off = 10 * 1.3e-5 * float(got.double().norm()) * float(d.norm()) / d.numel() ** 0.5
+        assert abs(difference - along) <= off + corners + 1e-10, (i, difference, along, off, corners)
 
 
 def test_adapters_forward_and_backward(handle):
@@ -610,3 +622,38 @@ def test_refusals(handle):
             assert err.value.status == ec.ERR_UNSUPPORTED
     torch.cuda.synchronize()
     assert bool((t == 0).all())
+
+
+@pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("trans", ["TNTT", "NNNN", "TNTN", "TTTT"])
+@pytest.mark.parametrize("N", [24, 150, 600])
+def test_an_adapter_that_is_not_finite_stays_with_its_columns(handle, trans, mode, N):
+    """What an adapter of one request holds does not reach the others, whichever kernels make the product."""
+    import torch
+    ec, gen = _ec(), _gen(13)
+    M, K, R = 300, 200, 12
+    sizes, index = [N // 6, N // 3, N // 6, N // 6], [0, 1, 2, 0]
+
+    def operand(rows, cols, t, **more):
+        return Field(rows, cols, gen=gen, **more) if t == "N" else Field(cols, rows, gen=gen, **more)
+
+    A, B = operand(M, K, trans[0]), operand(K, N, trans[1])
+    D, U = operand(R, K, trans[2], count=3), operand(M, R, trans[3], count=3)
+    results = []
+    for spoilt in (False, True):
+        if spoilt:
+            U.view()[1].fill_(float("nan"))
+            D.view()[2][3, 5] = float("inf")
+        H, C = Field(R, N, fill=7.0), Field(M, N, values=torch.full((1, N, M), 0.25, device="cuda"), fill=7.0)
+        handle.sgemm_adapters(_ops(trans[0]), _ops(trans[1]), M, N, K, 1.0, A.ptr(), A.ld, B.ptr(), B.ld, 4, _offsets(sizes, 2),
+                              torch.tensor(index, dtype=torch.int32, device="cuda"), 3, R, _ops(trans[2]), D.ptr(), D.ld, D.stride,
+                              _ops(trans[3]), U.ptr(), U.ld, U.stride, None, H.ptr(), H.ld, 2.0, C.ptr(), C.ld, _mode(mode))
+        torch.cuda.synchronize()
+        results.append((C.view()[0].clone(), H.view()[0].clone()))
+    at = np.cumsum([2, *sizes])
+    others = [*range(at[0]), *range(at[0], at[1]), *range(at[3], N)]
+    (clean, h_clean), (bad, h_bad) = results
+    assert torch.equal(clean[others], bad[others]) and torch.equal(h_clean[others], h_bad[others])
+    assert bool(torch.isnan(bad[at[1]:at[2]]).all())
+    assert torch.equal(h_clean[at[1]:at[2]], h_bad[at[1]:at[2]])
+    assert not bool(torch.isfinite(bad[at[2]:at[3]]).all(dim=1).any())
