@@ -62,11 +62,33 @@ ecgemm_status_t launch_grouped(ecgemm_handle_t h, ecgemm_mode_t mode, bool depth
 }
 
 // The kernels for few columns to a group (narrow_kernel.hpp).
-constexpr int64_t kNarrowMeanColumns = 32, kAdapterDownMeanColumns = 8, kNarrowProjectionColumns = 64;
+constexpr int64_t kAdapterDownMeanColumns = 8, kNarrowProjectionColumns = 96;
 constexpr int64_t kNarrowTallBlocks = 256;
 constexpr int64_t kAdapterOneLaunchDepth = 8192, kAdapterOneLaunchChunks = 8;
+
+// Whether ecgemm_sgemm_grouped runs on narrow_kernel, by what either kernel is estimated to take (us), all groups taken as
+// equal:
+//   tiles: 6, and the larger of what their rounds over the chip take (0.95 a chunk of 64 in FP16 mode, 1.5 BF16) and of
+//   reading A at 4.1 TB/s.
+//   narrow: 4, and a pass over A for every 32 columns of a group, at 4.7 TB/s or, where there are too few blocks for that, at
+//   what a block needs for the depth (2.9 per 1024; 9.3 where the rows are contiguous, and a block takes 64).
+// Tiles / narrow measured, FP16, A with the depth contiguous: M = K = 4096, one group of 32 columns 66.9 / 15.8, 64 67.9 /
+// 29.5, 128 65.2 / 55.2; eight groups of 8 127 / 94, 32 130 / 113, 48 132 / 185; 64 groups, 1536 x 2048, of 8 192 / 139, 32
+// 198 / 191, 48 202 / 306; eight, 768 x 1024, of 8 23.9 / 6.8, 96 26.4 / 22.9, 128 24.3 / 29.3; 4096 x 512 of 8 20.3 / 18.1, 32
+// 21.7 / 25.5; four, 512 x 8192, of 96 122 / 74, 128 121 / 98; rows contiguous: 4096 x 4096, one of 32 72 / 42, 64 72 / 80; eight of
+// 32 121 / 109, 64 124 / 197.  At worst 2048 x 2048, sixteen of 32, 55.5 / 60.6, which it takes narrow.
+bool narrow_is_faster(bool depth_a, int64_t groups, int64_t M, int64_t N, int64_t K, ecgemm_mode_t mode) {
+  const double bytes = 4.0 * groups * M * K, columns = (double)N / groups;
+  if (columns > kGroupedTile) return false;  // (not measured)
+  const double rounds = std::ceil((double)tiles_of(M) * groups * std::ceil(columns / kGroupedTile) / kPlanComputeUnits);
+  const double tiles_us = 6.0 + std::max(rounds * (K / 64.0) * (mode == ECGEMM_MODE_FP16_SPLIT ? 0.95 : 1.5), bytes / 4.1e6);
+  const double pass_us = std::max(bytes / 4.7e6, K / 1024.0 * (depth_a ? 2.9 : 9.3));
+  return 4.0 + std::ceil(columns / kNarrowColumns) * pass_us < tiles_us;
+}
+
 // Blocks of 16 rows the operand that is read once is taken in: four where its rows are contiguous, else two where that leaves
-// enough blocks and there are enough columns for it to matter.
+// enough blocks and there are enough columns for it to matter (4096 deep times 32 columns, 8192 rows 49.6 us / 33.8 with 32 rows
+// a block, 4096 rows 25.5 / 33.5).
 int narrow_fr(bool depth, int64_t groups, int64_t rows, int64_t columns) {
   return !depth ? 4 : columns > 16 && groups * ((rows + 31) / 32) >= kNarrowTallBlocks ? 2 : 1;
 }
@@ -138,7 +160,7 @@ ecgemm_status_t ecgemm_sgemm_grouped(ecgemm_handle_t handle, ecgemm_op_t transA,
   }
   const OnDeviceOf device(h);
   if (device.error != hipSuccess) return hip_fail(h, device.error, "hipSetDevice");
-  if (N <= kNarrowMeanColumns * groups && narrow_fits(groups, M)) {
+  if (narrow_is_faster(transA == ECGEMM_OP_T, groups, M, N, K, mode) && narrow_fits(groups, M)) {
     NarrowParams np{};
     np.A = A, np.lda = lda, np.stride_a = strideA;
     np.B = B, np.ldb = ldb;

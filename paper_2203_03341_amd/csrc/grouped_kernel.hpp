@@ -97,6 +97,17 @@ struct GroupedOperand {
   unsigned lane_bytes[DEPTH ? UNITS : 1];
   float factor;
 
+  // The place of a row within a half of 32 (see wide_lds_slot).  Where 16 lanes write at once they hold two rows of eight
+  // octets each (chunks of 64), rows contiguous four rows apart: place_in_half sends those to different banks.  In chunks of 32
+  // they hold four rows of four octets, or every other row of 32: bits 1 and 0 of the row become bits 3 and 2 of the place
+  // for the one, and bit 4 joins bit 0 for the other.  (With place_in_half a third of the LDS cycles of a BF16 call were
+  // conflicts.)
+  __device__ __forceinline__ static int place_of(int r) {
+    return K_STEPS == 4 ? place_in_half(r) : (r & 16) | (r & 2) << 2 | ((r ^ r >> 4) & 1) << 2 | (r & 8) >> 2 | (r & 4) >> 2;
+  }
+  __device__ __forceinline__ static int row_of_place(int q) {
+    return K_STEPS == 4 ? row_at_place(q) : (q & 16) | (q & 8) >> 2 | ((q >> 2 ^ q >> 4) & 1) | (q & 2) << 2 | (q & 1) << 2;
+  }
   __device__ __forceinline__ static int lds_slot(int row_block, int place, int octet) {
     return (row_block * K_STEPS + (octet >> 1)) * NP * 1024 + (octet & 1) * 512 + ((place + octet) & 31) * 16;
   }
@@ -223,7 +234,7 @@ struct GroupedOperand {
   }
   __device__ __forceinline__ void write(const uint4_t (&parts)[NP], int u, char* region) const {
     const int r = unit_row(u);
-    char* at = region + lds_slot(r >> 5, place_in_half(r & 31), octet);
+    char* at = region + lds_slot(r >> 5, place_of(r & 31), octet);
 #pragma unroll
     for (int q = 0; q < NP; ++q) *reinterpret_cast<uint4_t*>(at + q * 1024) = parts[q];
   }
@@ -659,8 +670,8 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_kernel(const Group
     // (the lane hidden from the optimizer: it would work out the columns' offsets before the first tile and keep them all)
     int lane_here = lane;
     asm volatile("" : "+v"(lane_here));
-    const int tile_row = wave_m * 64 + row_at_place(lane_here & 31);
-    auto tile_column = [&](int j, int v) { return wave_n * 64 + j * 32 + row_at_place(8 * (v / 4) + 4 * (lane_here >> 5) + v % 4); };
+    const int tile_row = wave_m * 64 + OperandA::row_of_place(lane_here & 31);
+    auto tile_column = [&](int j, int v) { return wave_n * 64 + j * 32 + OperandA::row_of_place(8 * (v / 4) + 4 * (lane_here >> 5) + v % 4); };
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int r = tile_row + i * 32;
