@@ -334,8 +334,9 @@ ecgemm_status_t ecgemm_product(ecgemm_handle_t handle, int64_t M, int64_t N, int
  *
  * Both modes of the method (ECGEMM_ERR_UNSUPPORTED for the others and for ECGEMM_MODE_AUTO), and the handle's pre-scaling
  * (ecgemm_set_scaling).  A forced kernel shape and the timing switch do not matter.  Leading dimensions of the operands up
- * to 2^21; M, N, K and the number of groups below 2^31.  No workspace is needed, and each call runs on the handle's device
- * whichever one is current.
+ * to 2^21; M, N, K and the number of groups below 2^31.  Calls of few output tiles and a great depth cut the depth into
+ * slices and put their sums into the handle's workspace, at most ECGEMM_GROUPED_WORKSPACE_BYTES of it; the others need none.
+ * Each call runs on the handle's device whichever one is current.
  *
  * ecgemm_sgemm_grouped, groups of columns (a layer of experts; with transA the other way round its input's gradient):
  *     C(:, j) <- alpha * op(A_g) * op(B)(:, j) + beta * C(:, j)      for every column j of every group g
@@ -348,6 +349,7 @@ ecgemm_status_t ecgemm_product(ecgemm_handle_t handle, int64_t M, int64_t N, int
  *
  * beta == 0: C is not read.  K == 0 or alpha == 0: A and B are not read.  C must not overlap A or B.
  */
+#define ECGEMM_GROUPED_WORKSPACE_BYTES ((size_t)16 << 20)
 ecgemm_status_t ecgemm_sgemm_grouped(ecgemm_handle_t handle, ecgemm_op_t transA, ecgemm_op_t transB, int64_t groups,
                                      int64_t M, int64_t N, int64_t K, float alpha, const float *A, int64_t lda,
                                      int64_t strideA, const float *B, int64_t ldb, const int64_t *offsets, float beta,

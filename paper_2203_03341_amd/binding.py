@@ -102,6 +102,7 @@ _lib = _load()
 
 
 NOALLOC_WORKSPACE_BYTES = 64 << 20      # ECGEMM_NOALLOC_WORKSPACE_BYTES
+GROUPED_WORKSPACE_BYTES = 16 << 20      # ECGEMM_GROUPED_WORKSPACE_BYTES
 
 
 class EcgemmError(RuntimeError):

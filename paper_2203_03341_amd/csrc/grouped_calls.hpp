@@ -36,6 +36,14 @@ int64_t most_grouped_tiles(bool along_depth, int64_t groups, int64_t M, int64_t 
   return along_depth ? g * tiles_of(M) * tiles_of(N) : tiles_of(M) * (N / kGroupedTile + std::min(g, N));
 }
 
+// Slices of the depth: where the tiles are few, as many as fill the chip, 512 deep at least, and only if that saves more than
+// the 7 us that adding them up takes.  At most 256 tiles of partial sums: ECGEMM_GROUPED_WORKSPACE_BYTES.
+int grouped_slices(int64_t tiles, int64_t depth) {
+  const int64_t slices = std::min<int64_t>(kPlanComputeUnits / std::max<int64_t>(tiles, 1), std::min<int64_t>(depth / 512, 64));
+  return slices >= 2 && depth / 64.0 * (1.0 - 1.0 / slices) * 0.95 > 8.0 ? (int)slices : 1;
+}
+static_assert((size_t)kPlanComputeUnits * kGroupedTile * kGroupedTile * sizeof(float) == ECGEMM_GROUPED_WORKSPACE_BYTES, "partial sums");
+
 // Everything about the call is checked; gp.groups and what goes with it is filled in here.
 ecgemm_status_t launch_grouped(ecgemm_handle_t h, ecgemm_mode_t mode, bool depth_a, bool depth_b, int64_t groups, GroupedParams gp) {
   const bool scaled = h->log2_scale_a != 0 || h->log2_scale_b != 0;
@@ -54,9 +62,24 @@ ecgemm_status_t launch_grouped(ecgemm_handle_t h, ecgemm_mode_t mode, bool depth
     gp.A = whole.A + first * whole.stride_a;
     gp.C = whole.C + first * whole.stride_c;
     const int64_t tiles = most_grouped_tiles(gp.along_depth, gp.groups, gp.M, gp.N);
-    const int64_t grid = std::max(std::min<int64_t>(tiles, h->compute_units), (tiles + kGroupedTilesPerBlock - 1) / kGroupedTilesPerBlock);
+    gp.slices = grouped_slices(tiles, gp.along_depth ? gp.K / gp.groups : gp.K);
+    gp.partial_tiles = tiles;
+    gp.partials = nullptr;
+    if (gp.slices > 1) {
+      char* ws = nullptr;
+      const ecgemm_status_t st = acquire_workspace(h, (size_t)gp.slices * tiles * kGroupedTile * kGroupedTile * sizeof(float), &ws);
+      if (st != ECGEMM_OK) return st;
+      h->auto_choice = nullptr;  // (the workspace held it)
+      gp.partials = reinterpret_cast<float*>(ws);
+    }
+    const int64_t items = tiles * gp.slices;
+    const int64_t grid = std::max(std::min<int64_t>(items, h->compute_units), (items + kGroupedTilesPerBlock - 1) / kGroupedTilesPerBlock);
     void* args[] = {&gp};
     ECGEMM_HIP(h, hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)grid), dim3(kGroupedThreads), args, 0, h->stream));
+    if (gp.slices > 1) {
+      hipLaunchKernelGGL(grouped_reduce_kernel, dim3((unsigned)(16 * tiles)), dim3(kGroupedThreads), 0, h->stream, gp);
+      ECGEMM_HIP(h, hipGetLastError());
+    }
   }
   return ECGEMM_OK;
 }
@@ -64,15 +87,15 @@ ecgemm_status_t launch_grouped(ecgemm_handle_t h, ecgemm_mode_t mode, bool depth
 // The kernels for few columns to a group (narrow_kernel.hpp).
 constexpr int64_t kAdapterDownMeanColumns = 8, kNarrowProjectionColumns = 96;
 constexpr int64_t kNarrowTallBlocks = 256;
-constexpr int64_t kAdapterOneLaunchDepth = 8192, kAdapterOneLaunchChunks = 8;
+constexpr int64_t kAdapterOneLaunchDepth = 6144, kAdapterOneLaunchChunks = 8, kAdapterOneLaunchTiles = 128;
 
 // Whether ecgemm_sgemm_grouped runs on narrow_kernel, by what either kernel is estimated to take (us), all groups taken as
 // equal:
-//   tiles: 6, and the larger of what their rounds over the chip take (0.95 a chunk of 64 in FP16 mode, 1.5 BF16) and of
-//   reading A at 4.1 TB/s.
+//   tiles: 6, and the larger of what their rounds over the chip take (0.95 a chunk of 64 in FP16 mode, 1.5 BF16; less by the
+//   slices of the depth, which cost 7 to add up) and of reading A at 4.1 TB/s.
 //   narrow: 4, and a pass over A for every 32 columns of a group, at 4.7 TB/s or, where there are too few blocks for that, at
 //   what a block needs for the depth (2.9 per 1024; 9.3 where the rows are contiguous, and a block takes 64).
-// Tiles / narrow measured, FP16, A with the depth contiguous: M = K = 4096, one group of 32 columns 66.9 / 15.8, 64 67.9 /
+// Tiles without slices / narrow measured, FP16, A with the depth contiguous: M = K = 4096, one group of 32 columns 66.9 / 15.8, 64 67.9 /
 // 29.5, 128 65.2 / 55.2; eight groups of 8 127 / 94, 32 130 / 113, 48 132 / 185; 64 groups, 1536 x 2048, of 8 192 / 139, 32
 // 198 / 191, 48 202 / 306; eight, 768 x 1024, of 8 23.9 / 6.8, 96 26.4 / 22.9, 128 24.3 / 29.3; 4096 x 512 of 8 20.3 / 18.1, 32
 // 21.7 / 25.5; four, 512 x 8192, of 96 122 / 74, 128 121 / 98; rows contiguous: 4096 x 4096, one of 32 72 / 42, 64 72 / 80; eight of
@@ -81,7 +104,9 @@ bool narrow_is_faster(bool depth_a, int64_t groups, int64_t M, int64_t N, int64_
   const double bytes = 4.0 * groups * M * K, columns = (double)N / groups;
   if (columns > kGroupedTile) return false;  // (not measured)
   const double rounds = std::ceil((double)tiles_of(M) * groups * std::ceil(columns / kGroupedTile) / kPlanComputeUnits);
-  const double tiles_us = 6.0 + std::max(rounds * (K / 64.0) * (mode == ECGEMM_MODE_FP16_SPLIT ? 0.95 : 1.5), bytes / 4.1e6);
+  const int slices = grouped_slices(most_grouped_tiles(false, groups, M, N), K);
+  const double chunks = (K / 64.0) * (mode == ECGEMM_MODE_FP16_SPLIT ? 0.95 : 1.5) / slices;
+  const double tiles_us = 6.0 + std::max(rounds * chunks, bytes / 4.1e6) + (slices > 1 ? 7.0 : 0.0);
   const double pass_us = std::max(bytes / 4.7e6, K / 1024.0 * (depth_a ? 2.9 : 9.3));
   return 4.0 + std::ceil(columns / kNarrowColumns) * pass_us < tiles_us;
 }
@@ -344,11 +369,16 @@ ecgemm_status_t ecgemm_sgemm_adapters(ecgemm_handle_t handle, ecgemm_op_t transA
     np.adapter_offsets = offsets, np.adapter_groups = groups, np.index = index, np.matrices = (int)adapters;
     return launch_narrow(h, transA == ECGEMM_OP_T, depth_b, np);
   }
-  // Projection and adapters in one launch, where both matrices and H are laid out alike (see grouped_kernel).
+  // Projection and adapters in one launch, where both matrices and H are laid out alike (see grouped_kernel), there are tiles
+  // enough for half the chip, no more than a few adapters meet in a tile, and the projection is not so deep that splitting
+  // first outweighs two passes over C.  Whole calls so / with C written first and the projection added, us, FP16, M x N x K,
+  // rank, groups: 4096^3, 16, 4 429 / 438, 64, 64 443 / 466; 4096 x 1024 x 4096, 16, 4 122 / 133, x 512 89 / 88, x 128 95 / 57; 1024 x
+  // 2048 x 1024, 16, 4 43 / 51, x 512 37 / 33; 2048 x 6000 x 5120, 64, 4 452 / 524; 8192 x 4096 x 8192, 32, 4 1534 / 1480; BF16 4096^3,
+  // 16, 4 610 / 665; 2049 x 1040 x 1500, 20, 61 76 / 100.
   const int64_t chunk = mode == ECGEMM_MODE_FP16_SPLIT ? 64 : 32, added_chunks = (1 + kGroupedTile * groups / N) * ((rank + chunk - 1) / chunk);
   const int64_t tiles = tiles_of(M) * tiles_of(N);
   if (project && transA == transU && depth_b && groups <= kGroupsPerLaunch && lda <= kGroupedLargestLd && ldb <= kGroupedLargestLd &&
-      h->log2_scale_a == 0 && h->log2_scale_b == 0 && K <= kAdapterOneLaunchDepth && added_chunks <= kAdapterOneLaunchChunks) {
+      h->log2_scale_a == 0 && h->log2_scale_b == 0 && K <= kAdapterOneLaunchDepth && tiles >= kAdapterOneLaunchTiles && added_chunks <= kAdapterOneLaunchChunks) {
     GroupedParams gp{};
     gp.A = A, gp.lda = lda;
     gp.B = B, gp.ldb = ldb;
@@ -360,6 +390,7 @@ ecgemm_status_t ecgemm_sgemm_adapters(ecgemm_handle_t handle, ecgemm_op_t transA
     gp.U = U, gp.ldu = ldu, gp.stride_u = strideU, gp.rank = rank;
     gp.H = H, gp.ldh = ldh;
     gp.prescale_a = gp.prescale_b = gp.out_scale = 1.0f;
+    gp.slices = 1;
     gp.alpha = alpha, gp.beta = beta;
     const bool depth_a = transA == ECGEMM_OP_T;
     const grouped_fn_t kernel = mode == ECGEMM_MODE_FP16_SPLIT

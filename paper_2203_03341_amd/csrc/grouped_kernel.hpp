@@ -47,6 +47,11 @@ struct GroupedParams {
   int64_t ldu, stride_u, rank;
   const float* H;
   int64_t ldh;
+  // slices > 1 (not ADAPTERS): every tile's depth is cut into that many items, whose sums go to partials[slice][tile][column][row]
+  // of `partial_tiles` tiles a slice, for grouped_reduce_kernel to add up
+  int slices;
+  int64_t partial_tiles;
+  float* partials;
   float prescale_a, prescale_b;  // powers of two applied before the split
   float out_scale;               // 1 / (prescale_a prescale_b)
   float alpha, beta;
@@ -62,6 +67,7 @@ struct GroupedItem {
   int rows, cols;  // of the tile that exist, at most 128
   int readable_rows, readable_cols;  // how many are in memory from the first one on, at most 128
   int m0, n0;      // adapters only: the tile's first row and column
+  float* partial;  // sliced tiles only, else null: where its sums go, 128 rows apart
 };
 
 // the value of the first lane, for what is the same in all of them
@@ -332,6 +338,76 @@ __device__ __forceinline__ void make_group_table(const GroupedParams& p, GroupTa
   __syncthreads();
 }
 
+// Item number `index`: the tile, and which slice of its depth.  Called by whole waves.
+template <bool DEPTH_A, bool DEPTH_B, bool ADAPTERS, int CHUNK>
+__device__ __forceinline__ GroupedItem grouped_item(const GroupedParams& p, const GroupTable& table, int index) {
+  const int lane = threadIdx.x & 63;
+  GroupedItem it;
+  it.partial = nullptr;
+  int slice = 0;
+  if (!ADAPTERS && p.slices > 1) {
+    const int tile = index / p.slices;
+    slice = index - tile * p.slices;
+    it.partial = p.partials + (slice * p.partial_tiles + tile) * (kGroupedTile * kGroupedTile);
+    index = tile;
+  }
+  int group, tile_m, tile_n;
+  if constexpr (ADAPTERS) {
+    tile_coordinates(index, p.tiles_m, p.tiles_n, 4, 1, tile_m, tile_n);
+    const int64_t m0 = (int64_t)tile_m * kGroupedTile, n0 = (int64_t)tile_n * kGroupedTile;
+    it.a = p.A + (DEPTH_A ? m0 * p.lda : m0);
+    it.b = p.B + (DEPTH_B ? n0 * p.ldb : n0);
+    it.c = p.C + m0 + n0 * p.ldc;
+    it.K = p.K;
+    it.rows = it.readable_rows = (int)(p.M - m0 < kGroupedTile ? p.M - m0 : kGroupedTile);
+    it.cols = it.readable_cols = (int)(p.N - n0 < kGroupedTile ? p.N - n0 : kGroupedTile);
+    it.m0 = (int)m0, it.n0 = (int)n0;
+  } else if (p.along_depth) {
+    const int tiles = p.tiles_m * p.tiles_n;
+    group = index / tiles;
+    tile_coordinates(index - group * tiles, p.tiles_m, p.tiles_n, 4, 1, tile_m, tile_n);
+    const int64_t begin = clamp_offset(uniform(p.offsets[group]), 0, p.K), end = clamp_offset(uniform(p.offsets[group + 1]), begin, p.K);
+    const int64_t m0 = (int64_t)tile_m * kGroupedTile, n0 = (int64_t)tile_n * kGroupedTile;
+    it.a = p.A + (DEPTH_A ? m0 * p.lda + begin : m0 + begin * p.lda);
+    it.b = p.B + (DEPTH_B ? n0 * p.ldb + begin : n0 + begin * p.ldb);
+    it.c = p.C + group * p.stride_c + m0 + n0 * p.ldc;
+    it.K = end - begin;
+    it.rows = it.readable_rows = (int)(p.M - m0 < kGroupedTile ? p.M - m0 : kGroupedTile);
+    it.cols = it.readable_cols = (int)(p.N - n0 < kGroupedTile ? p.N - n0 : kGroupedTile);
+  } else {
+    // the last group that starts at or before this tile: 64 lanes look at every 64th entry, then at 64 entries
+    const int column_tile = index / p.tiles_m;
+    const int block = __popcll(__builtin_amdgcn_ballot_w64(lane < kGroupsPerLaunch / 64 && table.first_tile[64 * (lane & (kGroupsPerLaunch / 64 - 1))] <= column_tile)) - 1;
+    group = 64 * block + __popcll(__builtin_amdgcn_ballot_w64(table.first_tile[64 * block + lane] <= column_tile)) - 1;
+    group = group < p.groups ? group : p.groups - 1;
+    const int begin = uniform(table.begin[group]), end = uniform(table.end[group]);
+    const int first_tile = uniform(table.first_tile[group]);
+    const int tiles_n = (end - begin + kGroupedTile - 1) / kGroupedTile;
+    const int64_t within = index - (int64_t)first_tile * p.tiles_m;
+    // (only offsets that decrease can bring a tile that does not exist: it has no columns and is passed over)
+    tile_m = 0, tile_n = tiles_n;
+    if (within < (int64_t)tiles_n * p.tiles_m) tile_coordinates((int)within, p.tiles_m, tiles_n, 4, 1, tile_m, tile_n);
+    const int64_t m0 = (int64_t)tile_m * kGroupedTile, n0 = begin + (int64_t)tile_n * kGroupedTile;
+    it.a = p.A + group * p.stride_a + (DEPTH_A ? m0 * p.lda : m0);
+    it.b = p.B + (DEPTH_B ? n0 * p.ldb : n0);
+    it.c = p.C + m0 + n0 * p.ldc;
+    it.rows = it.readable_rows = (int)(p.M - m0 < kGroupedTile ? p.M - m0 : kGroupedTile);
+    it.cols = (int)(end - n0 < kGroupedTile ? end - n0 : kGroupedTile);
+    it.readable_cols = (int)(p.N - n0 < kGroupedTile ? p.N - n0 : kGroupedTile);
+    it.K = it.cols > 0 ? p.K : 0;
+  }
+  if (!ADAPTERS && p.slices > 1) {
+    const int64_t chunks = (it.K + CHUNK - 1) / CHUNK, per_slice = (chunks + p.slices - 1) / p.slices, begin = slice * per_slice * CHUNK;
+    const int64_t left = it.K > begin ? it.K - begin : 0;
+    if (left > 0) {
+      it.a += DEPTH_A ? begin : begin * p.lda;
+      it.b += DEPTH_B ? begin : begin * p.ldb;
+    }
+    it.K = left < per_slice * CHUNK ? left : per_slice * CHUNK;
+  }
+  return it;
+}
+
 // ADAPTERS: a projection of all columns, op(A) op(B), with low-rank adapters.  The groups that a tile's columns belong to add a
 // chunk or two each to its depth: U_a's rows times H's columns, those of other groups taken as zero, times scale / alpha.  C is
 // written once; a pass of its own over C for the adapters costs as much as writing it twice more (4096 cubed, rank 32, 65 us
@@ -358,67 +434,21 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_kernel(const Group
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   int items;
   if (p.along_depth) {
-    items = p.groups * p.tiles_m * p.tiles_n;
+    items = p.groups * p.tiles_m * p.tiles_n * p.slices;
   } else if (ADAPTERS) {
     make_group_table(p, table, adapter_table, wave_sums);
     items = p.tiles_m * p.tiles_n;
   } else {
     make_group_table(p, table, nullptr, wave_sums);
-    const int64_t all = (int64_t)table.first_tile[kGroupsPerLaunch] * p.tiles_m, most = (int64_t)gridDim.x * kGroupedTilesPerBlock;
+    const int64_t all = (int64_t)table.first_tile[kGroupsPerLaunch] * p.tiles_m * p.slices;
+    // (more than the host has counted on there are only with offsets that decrease)
+    const int64_t most = p.slices > 1 ? p.partial_tiles * p.slices : (int64_t)gridDim.x * kGroupedTilesPerBlock;
     items = uniform((int)(all < most ? all : most));
   }
   // Each XCD takes a contiguous run of every round of tiles, whose patch shares rows of A and columns of B in its L2.
   const int position = (int)xcd_run_position(blockIdx.x, gridDim.x), step_items = (int)gridDim.x;
 
-  auto item_at = [&](int index) {
-    GroupedItem it;
-    int group, tile_m, tile_n;
-    if constexpr (ADAPTERS) {
-      tile_coordinates(index, p.tiles_m, p.tiles_n, 4, 1, tile_m, tile_n);
-      const int64_t m0 = (int64_t)tile_m * kGroupedTile, n0 = (int64_t)tile_n * kGroupedTile;
-      it.a = p.A + (DEPTH_A ? m0 * p.lda : m0);
-      it.b = p.B + (DEPTH_B ? n0 * p.ldb : n0);
-      it.c = p.C + m0 + n0 * p.ldc;
-      it.K = p.K;
-      it.rows = it.readable_rows = (int)(p.M - m0 < kGroupedTile ? p.M - m0 : kGroupedTile);
-      it.cols = it.readable_cols = (int)(p.N - n0 < kGroupedTile ? p.N - n0 : kGroupedTile);
-      it.m0 = (int)m0, it.n0 = (int)n0;
-    } else if (p.along_depth) {
-      const int tiles = p.tiles_m * p.tiles_n;
-      group = index / tiles;
-      tile_coordinates(index - group * tiles, p.tiles_m, p.tiles_n, 4, 1, tile_m, tile_n);
-      const int64_t begin = clamp_offset(uniform(p.offsets[group]), 0, p.K), end = clamp_offset(uniform(p.offsets[group + 1]), begin, p.K);
-      const int64_t m0 = (int64_t)tile_m * kGroupedTile, n0 = (int64_t)tile_n * kGroupedTile;
-      it.a = p.A + (DEPTH_A ? m0 * p.lda + begin : m0 + begin * p.lda);
-      it.b = p.B + (DEPTH_B ? n0 * p.ldb + begin : n0 + begin * p.ldb);
-      it.c = p.C + group * p.stride_c + m0 + n0 * p.ldc;
-      it.K = end - begin;
-      it.rows = it.readable_rows = (int)(p.M - m0 < kGroupedTile ? p.M - m0 : kGroupedTile);
-      it.cols = it.readable_cols = (int)(p.N - n0 < kGroupedTile ? p.N - n0 : kGroupedTile);
-    } else {
-      // the last group that starts at or before this tile: 64 lanes look at every 64th entry, then at 64 entries
-      const int column_tile = index / p.tiles_m;
-      const int block = __popcll(__builtin_amdgcn_ballot_w64(lane < kGroupsPerLaunch / 64 && table.first_tile[64 * (lane & (kGroupsPerLaunch / 64 - 1))] <= column_tile)) - 1;
-      group = 64 * block + __popcll(__builtin_amdgcn_ballot_w64(table.first_tile[64 * block + lane] <= column_tile)) - 1;
-      group = group < p.groups ? group : p.groups - 1;
-      const int begin = uniform(table.begin[group]), end = uniform(table.end[group]);
-      const int first_tile = uniform(table.first_tile[group]);
-      const int tiles_n = (end - begin + kGroupedTile - 1) / kGroupedTile;
-      const int64_t within = index - (int64_t)first_tile * p.tiles_m;
-      // (only offsets that decrease can bring a tile that does not exist: it has no columns and is passed over)
-      tile_m = 0, tile_n = tiles_n;
-      if (within < (int64_t)tiles_n * p.tiles_m) tile_coordinates((int)within, p.tiles_m, tiles_n, 4, 1, tile_m, tile_n);
-      const int64_t m0 = (int64_t)tile_m * kGroupedTile, n0 = begin + (int64_t)tile_n * kGroupedTile;
-      it.a = p.A + group * p.stride_a + (DEPTH_A ? m0 * p.lda : m0);
-      it.b = p.B + (DEPTH_B ? n0 * p.ldb : n0);
-      it.c = p.C + m0 + n0 * p.ldc;
-      it.rows = it.readable_rows = (int)(p.M - m0 < kGroupedTile ? p.M - m0 : kGroupedTile);
-      it.cols = (int)(end - n0 < kGroupedTile ? end - n0 : kGroupedTile);
-      it.readable_cols = (int)(p.N - n0 < kGroupedTile ? p.N - n0 : kGroupedTile);
-      it.K = it.cols > 0 ? p.K : 0;
-    }
-    return it;
-  };
+  auto item_at = [&](int index) { return grouped_item<DEPTH_A, DEPTH_B, ADAPTERS, OperandA::CHUNK>(p, table, index); };
   auto chunks_of = [&](const GroupedItem& it) { return (int)((it.K + CHUNK - 1) / CHUNK); };
 
   // The adapters of a tile's columns, in the order of their groups: visit(group, first column, last column + 1).
@@ -672,33 +702,57 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_kernel(const Group
     asm volatile("" : "+v"(lane_here));
     const int tile_row = wave_m * 64 + OperandA::row_of_place(lane_here & 31);
     auto tile_column = [&](int j, int v) { return wave_n * 64 + j * 32 + OperandA::row_of_place(8 * (v / 4) + 4 * (lane_here >> 5) + v % 4); };
+    auto store_all = [&](auto whole_c) {
+      constexpr bool whole = decltype(whole_c)::value;
+      if (it.partial != nullptr) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int r = tile_row + i * 32;
-      if (r >= it.rows) continue;
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        float* dst = it.c + r;
-        auto store_all = [&](auto whole_c) {
-          constexpr bool whole = decltype(whole_c)::value;
-          if (p.beta != 0.0f) {
-            float c_in[16];
+          for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) c_in[v] = whole || mine(tile_column(j, v)) ? load_global(dst + tile_column(j, v) * p.ldc) : 0.0f;
+            for (int v = 0; v < 16; ++v)
+              if (whole || mine(tile_column(j, v))) store_partial(it.partial + tile_column(j, v) * kGroupedTile + tile_row + i * 32, acc_main[i][j][v]);
+        return;
+      }
+      if (p.beta != 0.0f) {
+        // (all that is added to is requested first, into the registers that the corrections have left, and without conditions:
+        // a row or column that does not exist reads the last one that does)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int r = tile_row + i * 32;
+          const float* from = it.c + (r < it.rows ? r : it.rows - 1);
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+              const int c = tile_column(j, v);
+              acc_corr[i][j][v] = load_global(from + (whole || c < it.cols ? c : it.cols - 1) * p.ldc);
+            }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float* dst = it.c + tile_row + i * 32;
+        if (tile_row + i * 32 >= it.rows) continue;
+        if (p.beta != 0.0f) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int v = 0; v < 16; ++v)
               if (whole || mine(tile_column(j, v)))
-                store_result(dst + tile_column(j, v) * p.ldc, scaled_sum(p.alpha, acc_main[i][j][v] * p.out_scale, p.beta, c_in[v]));
-          } else {
+                store_result(dst + tile_column(j, v) * p.ldc, scaled_sum(p.alpha, acc_main[i][j][v] * p.out_scale, p.beta, acc_corr[i][j][v]));
+        } else {
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int v = 0; v < 16; ++v)
               if (whole || mine(tile_column(j, v))) store_result(dst + tile_column(j, v) * p.ldc, p.alpha * (acc_main[i][j][v] * p.out_scale));
-          }
-        };
-        if (it.cols == kGroupedTile && (!ADAPTERS || (columns[0] & columns[1]) == ~0ull)) store_all(std::true_type{});
-        else store_all(std::false_type{});
+        }
       }
-    }
+    };
+    if (it.cols <= 0) return;
+    if (it.cols == kGroupedTile && (!ADAPTERS || (columns[0] & columns[1]) == ~0ull)) store_all(std::true_type{});
+    else store_all(std::false_type{});
   };
   // (one loop for both passes, so that what they do is in the program once.  In the second one, a tile with adapters is made
   // once for each of them and once without any, and the columns concerned are written: an adapter that is not finite has

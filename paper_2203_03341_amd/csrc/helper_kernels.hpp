@@ -1,6 +1,7 @@
-// The small kernels around the hot path: C <- beta C, exponent statistics for the pre-scaling helpers, and the two
-// diagnostic kernels that run bare matrix instructions.  Compiled with the host code (ecgemm.hip) only.
+// The small kernels around the hot path: C <- beta C, the sums of the grouped products' slices, exponent statistics for the
+// pre-scaling helpers, and the two diagnostic kernels that run bare matrix instructions.  Compiled with the host code (ecgemm.hip) only.
 #pragma once
+#include "grouped_kernel.hpp"
 #include "product_kernel.hpp"
 
 namespace ecgemm {
@@ -361,5 +362,36 @@ __global__ void __launch_bounds__(kMeasureThreads) measure_rows_kernel(const Mea
 
 // The choice from what measure_rows_kernel left, in a launch of its own (for calls whose candidates are not one kernel).
 __global__ void __launch_bounds__(256) choose_from_rows_kernel(const RowSums sums) { choose_from_rows(sums, true); }
+
+// The sums of tiles whose depth is cut into slices, in ascending order; then alpha and beta.  Block b: a sixteenth (b % 16) of
+// tile b / 16.
+__global__ void __launch_bounds__(kGroupedThreads) grouped_reduce_kernel(const GroupedParams params) {
+  __shared__ GroupTable table;
+  __shared__ int wave_sums[kGroupedThreads / 64];
+  GroupedParams p = params;
+  int64_t tiles = (int64_t)p.groups * p.tiles_m * p.tiles_n;
+  if (!p.along_depth) {
+    make_group_table(p, table, nullptr, wave_sums);
+    tiles = (int64_t)uniform(table.first_tile[kGroupsPerLaunch]) * p.tiles_m;
+  }
+  const int64_t tile = blockIdx.x / 16;
+  if (tile >= tiles) return;
+  p.slices = 1;  // (the item is the whole tile)
+  const GroupedItem it = grouped_item<false, false, false, 64>(p, table, (int)tile);
+  const int row = threadIdx.x % kGroupedTile, first = (int)(blockIdx.x % 16) * 8 + threadIdx.x / kGroupedTile;
+  if (row >= it.rows) return;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int column = first + 4 * i;
+    if (column >= it.cols) continue;
+    const float* from = p.partials + tile * (kGroupedTile * kGroupedTile) + column * kGroupedTile + row;
+    float c = 0.0f;
+#pragma unroll 4
+    for (int s = 0; s < params.slices; ++s) c += load_global(from + s * p.partial_tiles * (kGroupedTile * kGroupedTile));
+    float* dst = it.c + row + column * p.ldc;
+    c *= p.out_scale;
+    store_result(dst, p.beta != 0.0f ? scaled_sum(p.alpha, c, p.beta, load_global(dst)) : p.alpha * c);
+  }
+}
 
 }  // namespace ecgemm

@@ -657,3 +657,49 @@ def test_an_adapter_that_is_not_finite_stays_with_its_columns(handle, trans, mod
     assert bool(torch.isnan(bad[at[1]:at[2]]).all())
     assert torch.equal(h_clean[at[1]:at[2]], h_bad[at[1]:at[2]])
     assert not bool(torch.isfinite(bad[at[2]:at[3]]).all(dim=1).any())
+
+
+@pytest.mark.parametrize("mode", MODES)
+def test_deep_products_of_few_tiles_are_added_up_from_slices(handle, mode):
+    """Slices of the depth through the workspace: every storage order, ragged depths, nothing in some groups, and a caller's
+    workspace of the promised size."""
+    import torch
+    ec = _ec()
+    workspace = torch.full((ec.GROUPED_WORKSPACE_BYTES // 4 + 64,), 3.0, device="cuda")
+    for trans in ("TN", "NT", "NN", "TT"):
+        _run_columns(handle, trans, mode, 200, 2500, [140, 0, 300], start=1, behind=3, alpha=1.5, beta=-0.5, pad=(1, 2, 3))
+        _run_depth(handle, trans, mode, 130, 90, [2000, 3, 0, 5001], behind=7, alpha=1.5, beta=-0.5, pad=(1, 2, 3))
+    own = ec.Handle()
+    own.set_stream(torch.cuda.current_stream().cuda_stream)
+    own.set_workspace(workspace, ec.GROUPED_WORKSPACE_BYTES)
+    _run_depth(own, "NT", mode, 1000, 1000, [9000])
+    _run_depth(own, "NT", mode, 100, 100, [40000])
+    _run_columns(own, "TN", mode, 128, 4100, [256])
+    torch.cuda.synchronize()
+    assert bool((workspace[ec.GROUPED_WORKSPACE_BYTES // 4:] == 3.0).all())
+    own.set_workspace(workspace, 256)
+    with pytest.raises(ec.EcgemmError) as err:
+        _run_depth(own, "NT", mode, 100, 100, [40000])
+    assert err.value.status == ec.ERR_ALLOC
+    own.destroy()
+
+
+@pytest.mark.parametrize("mode", MODES)
+def test_values_that_are_not_finite_in_slices_and_few_columns(handle, mode):
+    """A NaN in one slice of the depth, and with few columns, stays in its row; the rest is as without it, bit for bit."""
+    import torch
+    ec, gen = _ec(), _gen(21)
+    for M, N, K in ((150, 260, 3000), (150, 9, 300)):
+        A, B = Field(K, M, count=2, gen=gen), Field(K, N, gen=gen)
+        sizes, results = [N // 2, N - N // 2], []
+        for spoilt in (False, True):
+            if spoilt:
+                A.view()[1, 77, K - 5] = float("nan")
+            C = Field(M, N, values=torch.full((1, N, M), 0.25, device="cuda"), fill=7.0)
+            handle.sgemm_grouped(ec.OP_T, ec.OP_N, 2, M, N, K, 1.0, A.ptr(), A.ld, A.stride, B.ptr(), B.ld, _offsets(sizes), 2.0, C.ptr(), C.ld,
+                                 _mode(mode))
+            torch.cuda.synchronize()
+            results.append(C.view()[0].clone())
+        touched = torch.zeros_like(results[0], dtype=torch.bool)
+        touched[N // 2:, 77] = True
+        assert torch.equal(results[0][~touched], results[1][~touched]) and bool(torch.isnan(results[1][touched]).all())
