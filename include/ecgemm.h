@@ -348,6 +348,10 @@ ecgemm_status_t ecgemm_product(ecgemm_handle_t handle, int64_t M, int64_t N, int
  *   op(A) is M x K, op(B) is K x N, C_g = C + g strideC is M x N.  A group without any depth gives C_g <- beta * C_g.
  *
  * beta == 0: C is not read.  K == 0 or alpha == 0: A and B are not read.  C must not overlap A or B.
+ *
+ * Groups of few columns (a decoding step) are computed in FP32 on the matrix unit, whichever mode is asked for: such a call
+ * is bound by reading A, and its result is at least as exact.  It follows from the sizes alone whether a call is.  An
+ * infinite or NaN value reaches the row of C or the columns that it is multiplied into, and nothing else.
  */
 #define ECGEMM_GROUPED_WORKSPACE_BYTES ((size_t)16 << 20)
 ecgemm_status_t ecgemm_sgemm_grouped(ecgemm_handle_t handle, ecgemm_op_t transA, ecgemm_op_t transB, int64_t groups,
@@ -374,6 +378,8 @@ ecgemm_status_t ecgemm_sgemm_grouped_depth(ecgemm_handle_t handle, ecgemm_op_t t
  *      pass needs it: with G the gradient of C, the gradient of op(B) is this same call on G with op(A)^T in A's place, U^T in
  *      D's and D^T in U's, which leaves U^T G in its H; the gradients of U and D are ecgemm_sgemm_grouped_depth of G with H,
  *      and of that call's H with B.
+ * H times scales[a] / alpha is an operand like B: in FP16 mode it should lie in the window of the FP16 pair as well.  An adapter
+ * that holds infinite or NaN values reaches its own columns only.
  * rank at most 1024; adapters below 2^31.  The projection uses the handle's workspace as ecgemm_sgemm does
  * (ecgemm_workspace_size for M, N, K says how much).  C and H must not overlap each other or anything else.
  */

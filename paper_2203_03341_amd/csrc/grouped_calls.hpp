@@ -325,6 +325,27 @@ ecgemm_status_t ecgemm_sgemm_adapters(ecgemm_handle_t handle, ecgemm_op_t transA
     if (M == 0) return ECGEMM_OK;
     return sgemm_common(h, transA, transB, M, N, K, alpha, A, lda, B, ldb, beta, C, ldc, mode, nullptr, nullptr, kWorkspaceOfHandle);
   }
+  const bool narrow = project && N <= kNarrowProjectionColumns && lda <= kGroupedLargestLd;
+  // Projection and adapters in one launch, where both matrices and H are laid out alike (see grouped_kernel), there are tiles
+  // enough for half the chip, no more than a few adapters meet in a tile, and the projection is not so deep that splitting
+  // first outweighs two passes over C.  Whole calls so / with C written first and the projection added, us, FP16, M x N x K,
+  // rank, groups: 4096^3, 16, 4 429 / 438, 64, 64 443 / 466; 4096 x 1024 x 4096, 16, 4 122 / 133, x 512 89 / 88, x 128 95 / 57; 1024 x
+  // 2048 x 1024, 16, 4 43 / 51, x 512 37 / 33; 2048 x 6000 x 5120, 64, 4 452 / 524; 8192 x 4096 x 8192, 32, 4 1534 / 1480; BF16 4096^3,
+  // 16, 4 610 / 665; 2049 x 1040 x 1500, 20, 61 76 / 100.
+  const int64_t chunk = mode == ECGEMM_MODE_FP16_SPLIT ? 64 : 32, added_chunks = (1 + kGroupedTile * groups / N) * ((rank + chunk - 1) / chunk);
+  const int64_t tiles = tiles_of(M) * tiles_of(N);
+  const bool one_launch = project && !narrow && transA == transU && depth_b && groups <= kGroupsPerLaunch && lda <= kGroupedLargestLd &&
+                          h->log2_scale_a == 0 && h->log2_scale_b == 0 && K <= kAdapterOneLaunchDepth && tiles >= kAdapterOneLaunchTiles && added_chunks <= kAdapterOneLaunchChunks &&
+                          std::fabs(alpha) >= 0x1p-16f && std::fabs(alpha) <= 0x1p16f;  // (H is multiplied by scales / alpha)
+  if (project && !narrow && !one_launch) {  // what the projection would refuse is refused before anything is enqueued
+    st = check_sizes(h, M, N, K, mode, 4);
+    if (st != ECGEMM_OK) return st;
+    const Plan pl = make_plan(M, N, K, mode, h->shape, kOneLaunchSliced);
+    if (!pl.shape) return no_plan(h, pl, "ecgemm_sgemm_adapters");
+    char* ws = nullptr;
+    st = acquire_workspace(h, pl.total_bytes, &ws);
+    if (st != ECGEMM_OK) return st;
+  }
   // H = op(D) op(B), zero in every column without an adapter: few columns to a group, the adapters are read once, else B is
   if (N < kAdapterDownMeanColumns * groups && narrow_fits(groups, rank)) {
     NarrowParams down{};
@@ -356,7 +377,7 @@ ecgemm_status_t ecgemm_sgemm_adapters(ecgemm_handle_t handle, ecgemm_op_t transA
                                   dim3(kNarrowThreads), args, 0, h->stream));
   }
   if (M == 0) return ECGEMM_OK;
-  if (project && N <= kNarrowProjectionColumns && lda <= kGroupedLargestLd) {
+  if (narrow) {
     // few columns: the projection reads its matrix once, and adds the adapters to what it writes
     NarrowParams np{};
     np.A = A, np.lda = lda;
@@ -369,16 +390,7 @@ ecgemm_status_t ecgemm_sgemm_adapters(ecgemm_handle_t handle, ecgemm_op_t transA
     np.adapter_offsets = offsets, np.adapter_groups = groups, np.index = index, np.matrices = (int)adapters;
     return launch_narrow(h, transA == ECGEMM_OP_T, depth_b, np);
   }
-  // Projection and adapters in one launch, where both matrices and H are laid out alike (see grouped_kernel), there are tiles
-  // enough for half the chip, no more than a few adapters meet in a tile, and the projection is not so deep that splitting
-  // first outweighs two passes over C.  Whole calls so / with C written first and the projection added, us, FP16, M x N x K,
-  // rank, groups: 4096^3, 16, 4 429 / 438, 64, 64 443 / 466; 4096 x 1024 x 4096, 16, 4 122 / 133, x 512 89 / 88, x 128 95 / 57; 1024 x
-  // 2048 x 1024, 16, 4 43 / 51, x 512 37 / 33; 2048 x 6000 x 5120, 64, 4 452 / 524; 8192 x 4096 x 8192, 32, 4 1534 / 1480; BF16 4096^3,
-  // 16, 4 610 / 665; 2049 x 1040 x 1500, 20, 61 76 / 100.
-  const int64_t chunk = mode == ECGEMM_MODE_FP16_SPLIT ? 64 : 32, added_chunks = (1 + kGroupedTile * groups / N) * ((rank + chunk - 1) / chunk);
-  const int64_t tiles = tiles_of(M) * tiles_of(N);
-  if (project && transA == transU && depth_b && groups <= kGroupsPerLaunch && lda <= kGroupedLargestLd && ldb <= kGroupedLargestLd &&
-      h->log2_scale_a == 0 && h->log2_scale_b == 0 && K <= kAdapterOneLaunchDepth && tiles >= kAdapterOneLaunchTiles && added_chunks <= kAdapterOneLaunchChunks) {
+  if (one_launch) {
     GroupedParams gp{};
     gp.A = A, gp.lda = lda;
     gp.B = B, gp.ldb = ldb;
@@ -412,7 +424,7 @@ ecgemm_status_t ecgemm_sgemm_adapters(ecgemm_handle_t handle, ecgemm_op_t transA
   up.scales = scales, up.beta = beta;
   up.row_blocks = (int)((M + 255) / 256);
   hipLaunchKernelGGL((transU == ECGEMM_OP_T ? adapter_up_kernel<true> : adapter_up_kernel<false>),
-                     dim3((unsigned)(up.row_blocks * ((N + kNarrowColumns - 1) / kNarrowColumns))), dim3(256), 0, h->stream, up);
+                     dim3((unsigned)(up.row_blocks * ((N + kAdapterUpColumns - 1) / kAdapterUpColumns))), dim3(256), 0, h->stream, up);
   ECGEMM_HIP(h, hipGetLastError());
   if (!project) return ECGEMM_OK;
   return sgemm_common(h, transA, transB, M, N, K, alpha, A, lda, B, ldb, 1.0f, C, ldc, mode, nullptr, nullptr, kWorkspaceOfHandle);

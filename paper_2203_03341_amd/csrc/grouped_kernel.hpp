@@ -280,7 +280,9 @@ struct GroupedOperand {
   }
 };
 
-// The groups of a launch as a block keeps them: columns [begin, end) of each, and the number of 128-column tiles before it.
+// The groups of a launch as a block keeps them: [begin, end) of each along the columns or the depth, and the number of
+// 128-column tiles before it (columns only).  A block reads the offsets once: all its waves see the same ones, whatever
+// happens to them meanwhile, and pass the same barriers.
 struct GroupTable {
   int first_tile[kGroupsPerLaunch + 64];  // [groups] and everything behind it: the number of all tiles
   int begin[kGroupsPerLaunch], end[kGroupsPerLaunch];
@@ -291,8 +293,8 @@ struct AdapterTable {
   float scale[kGroupsPerLaunch];
 };
 __device__ __forceinline__ int64_t clamp_offset(int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; }
-// Called by all kGroupedThreads threads; ends with a barrier.  Offsets outside [0, N] or decreasing ones are clamped, so that
-// no tile ever reaches beyond the operands (the caller holds N <= 2^31 - 1).
+// Called by all kGroupedThreads threads; ends with a barrier.  Offsets outside [0, N] (or K) or decreasing ones are
+// clamped, so that no tile ever reaches beyond the operands (the caller holds N and K <= 2^31 - 1).
 __device__ __forceinline__ void make_group_table(const GroupedParams& p, GroupTable& table, AdapterTable* adapters, int* wave_sums) {
   constexpr int PER_THREAD = kGroupsPerLaunch / kGroupedThreads;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
@@ -302,7 +304,8 @@ __device__ __forceinline__ void make_group_table(const GroupedParams& p, GroupTa
     const int g = PER_THREAD * t + i;
     tiles[i] = 0;
     if (g < p.groups) {
-      const int64_t begin = clamp_offset(p.offsets[g], 0, p.N), end = clamp_offset(p.offsets[g + 1], begin, p.N);
+      const int64_t most = p.along_depth ? p.K : p.N;
+      const int64_t begin = clamp_offset(p.offsets[g], 0, most), end = clamp_offset(p.offsets[g + 1], begin, most);
       table.begin[g] = (int)begin, table.end[g] = (int)end;
       if (adapters != nullptr) {
         const int a = p.index[g], adapter = a >= 0 && a < p.matrices ? a : -1;
@@ -366,7 +369,7 @@ __device__ __forceinline__ GroupedItem grouped_item(const GroupedParams& p, cons
     const int tiles = p.tiles_m * p.tiles_n;
     group = index / tiles;
     tile_coordinates(index - group * tiles, p.tiles_m, p.tiles_n, 4, 1, tile_m, tile_n);
-    const int64_t begin = clamp_offset(uniform(p.offsets[group]), 0, p.K), end = clamp_offset(uniform(p.offsets[group + 1]), begin, p.K);
+    const int64_t begin = uniform(table.begin[group]), end = uniform(table.end[group]);
     const int64_t m0 = (int64_t)tile_m * kGroupedTile, n0 = (int64_t)tile_n * kGroupedTile;
     it.a = p.A + (DEPTH_A ? m0 * p.lda + begin : m0 + begin * p.lda);
     it.b = p.B + (DEPTH_B ? n0 * p.ldb + begin : n0 + begin * p.ldb);
@@ -434,6 +437,7 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_kernel(const Group
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   int items;
   if (p.along_depth) {
+    make_group_table(p, table, nullptr, wave_sums);
     items = p.groups * p.tiles_m * p.tiles_n * p.slices;
   } else if (ADAPTERS) {
     make_group_table(p, table, adapter_table, wave_sums);
@@ -696,6 +700,7 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_kernel(const Group
   // a lane owns one row per 32 x 32 block; register v of it is the matrix instruction's column 8 (v / 4) + 4 (lane / 32) + v % 4
   // ADAPTERS: `columns` of the tile's columns, a bit each
   auto write_tile = [&](const GroupedItem& it, const uint64_t (&columns)[2]) {
+    const float alpha = it.K > 0 ? p.alpha : 0.0f;  // (nothing to multiply: no infinity times zero)
     auto mine = [&](int c) { return c < it.cols && (!ADAPTERS || (columns[c >> 6] >> (c & 63) & 1) != 0); };
     // (the lane hidden from the optimizer: it would work out the columns' offsets before the first tile and keep them all)
     int lane_here = lane;
@@ -740,13 +745,13 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_kernel(const Group
 #pragma unroll
             for (int v = 0; v < 16; ++v)
               if (whole || mine(tile_column(j, v)))
-                store_result(dst + tile_column(j, v) * p.ldc, scaled_sum(p.alpha, acc_main[i][j][v] * p.out_scale, p.beta, acc_corr[i][j][v]));
+                store_result(dst + tile_column(j, v) * p.ldc, scaled_sum(alpha, acc_main[i][j][v] * p.out_scale, p.beta, acc_corr[i][j][v]));
         } else {
 #pragma unroll
           for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int v = 0; v < 16; ++v)
-              if (whole || mine(tile_column(j, v))) store_result(dst + tile_column(j, v) * p.ldc, p.alpha * (acc_main[i][j][v] * p.out_scale));
+              if (whole || mine(tile_column(j, v))) store_result(dst + tile_column(j, v) * p.ldc, alpha * (acc_main[i][j][v] * p.out_scale));
         }
       }
     };

@@ -369,11 +369,8 @@ __global__ void __launch_bounds__(kGroupedThreads) grouped_reduce_kernel(const G
   __shared__ GroupTable table;
   __shared__ int wave_sums[kGroupedThreads / 64];
   GroupedParams p = params;
-  int64_t tiles = (int64_t)p.groups * p.tiles_m * p.tiles_n;
-  if (!p.along_depth) {
-    make_group_table(p, table, nullptr, wave_sums);
-    tiles = (int64_t)uniform(table.first_tile[kGroupsPerLaunch]) * p.tiles_m;
-  }
+  make_group_table(p, table, nullptr, wave_sums);
+  const int64_t tiles = p.along_depth ? (int64_t)p.groups * p.tiles_m * p.tiles_n : (int64_t)uniform(table.first_tile[kGroupsPerLaunch]) * p.tiles_m;
   const int64_t tile = blockIdx.x / 16;
   if (tile >= tiles) return;
   p.slices = 1;  // (the item is the whole tile)
@@ -390,7 +387,8 @@ __global__ void __launch_bounds__(kGroupedThreads) grouped_reduce_kernel(const G
     for (int s = 0; s < params.slices; ++s) c += load_global(from + s * p.partial_tiles * (kGroupedTile * kGroupedTile));
     float* dst = it.c + row + column * p.ldc;
     c *= p.out_scale;
-    store_result(dst, p.beta != 0.0f ? scaled_sum(p.alpha, c, p.beta, load_global(dst)) : p.alpha * c);
+    const float alpha = it.K > 0 ? p.alpha : 0.0f;
+    store_result(dst, p.beta != 0.0f ? scaled_sum(alpha, c, p.beta, load_global(dst)) : alpha * c);
   }
 }
 

@@ -296,23 +296,33 @@ __global__ void __launch_bounds__(kNarrowThreads, DEPTH_A && FR == 1 ? 4 : 2) na
   const int64_t group = blockIdx.x / (unsigned)p.row_blocks;
   const int64_t m0 = (int64_t)(blockIdx.x % (unsigned)p.row_blocks) * ROWS;
   const int rows = (int)(p.M - m0 < ROWS ? p.M - m0 : ROWS);
-  int64_t begin = 0, end = p.N;
-  int matrix = 0;
-  if (p.offsets != nullptr) {
-    if (group >= p.groups) {  // columns in no group, before the first one and behind the last
-      const int64_t first = clamp_offset(uniform(p.offsets[0]), 0, p.N), last = clamp_offset(uniform(p.offsets[p.groups]), first, p.N);
-      for (int64_t i = threadIdx.x; i < (first + p.N - last) * rows; i += kNarrowThreads) {
-        const int64_t j = i / rows;
-        p.C[m0 + i % rows + (j < first ? j : j - first + last) * p.ldc] = 0.0f;
+  // (the offsets are read once for the block: all its waves pass the same barriers, whatever happens to them meanwhile)
+  __shared__ int64_t range[2];
+  __shared__ int chosen;
+  if (threadIdx.x == 0) {
+    range[0] = 0, range[1] = p.N, chosen = 0;
+    if (p.offsets != nullptr) {
+      const int64_t first = group < p.groups ? group : 0, last = group < p.groups ? group + 1 : p.groups;
+      range[0] = clamp_offset(p.offsets[first], 0, p.N);
+      range[1] = clamp_offset(p.offsets[last], range[0], p.N);
+      if (group < p.groups) {
+        chosen = (int)group;
+        if (p.index != nullptr) {
+          const int index = p.index[group];
+          chosen = index >= 0 && index < p.matrices ? index : -1;
+        }
       }
-      return;
     }
-    begin = clamp_offset(uniform(p.offsets[group]), 0, p.N), end = clamp_offset(uniform(p.offsets[group + 1]), begin, p.N);
-    matrix = (int)group;
-    if (p.index != nullptr) {
-      matrix = uniform(p.index[group]);
-      if (matrix < 0 || matrix >= p.matrices) matrix = -1;
+  }
+  __syncthreads();
+  const int64_t begin = uniform(range[0]), end = uniform(range[1]);
+  const int matrix = uniform(chosen);
+  if (p.offsets != nullptr && group >= p.groups) {  // columns in no group, before the first one and behind the last
+    for (int64_t i = threadIdx.x; i < (begin + p.N - end) * rows; i += kNarrowThreads) {
+      const int64_t j = i / rows;
+      p.C[m0 + i % rows + (j < begin ? j : j - begin + end) * p.ldc] = 0.0f;
     }
+    return;
   }
   const float* a = p.A + matrix * p.stride_a + (DEPTH_A ? m0 * p.lda : m0);
   for (int64_t n0 = begin; n0 < end; n0 += kNarrowColumns) {
@@ -322,7 +332,7 @@ __global__ void __launch_bounds__(kNarrowThreads, DEPTH_A && FR == 1 ? 4 : 2) na
     for (int i = threadIdx.x; i < ROWS * cols; i += kNarrowThreads) {
       const int r = i % ROWS, c = i / ROWS;
       if (r >= rows) continue;
-      float value = p.alpha * narrow_sum(sums, r, c);
+      float value = p.K > 0 ? p.alpha * narrow_sum(sums, r, c) : 0.0f;
       if (p.U != nullptr && adapter[c] >= 0) {
         const float* u = p.U + adapter[c] * p.stride_u + (p.u_depth ? (m0 + r) * p.ldu : m0 + r);
         const float* h = p.H + (n0 + c) * p.ldh;

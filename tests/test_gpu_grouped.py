@@ -703,3 +703,43 @@ def test_values_that_are_not_finite_in_slices_and_few_columns(handle, mode):
         touched = torch.zeros_like(results[0], dtype=torch.bool)
         touched[N // 2:, 77] = True
         assert torch.equal(results[0][~touched], results[1][~touched]) and bool(torch.isnan(results[1][touched]).all())
+
+
+def test_adapters_of_the_largest_rank_and_through_the_workspace(handle):
+    """Ranks beyond a few passes; and the way that takes the handle's workspace refuses a small one before it writes anything."""
+    import torch
+    ec = _ec()
+    for mode in MODES:
+        _run_adapters(handle, mode, 70, 40, 90, 1024, [20, 20], [1, 0], 2)
+        _run_adapters(handle, mode, 130, 300, 90, 1024, [200, 90], [1, 0], 2, trans="NNTN")
+    own = ec.Handle()
+    own.set_stream(torch.cuda.current_stream().cuda_stream)
+    small = torch.empty(256, dtype=torch.uint8, device="cuda")
+    own.set_workspace(small, 256)
+    H, C = torch.full((2000, 8), 7.0, device="cuda"), torch.full((2000, 2000), 7.0, device="cuda")
+    x, W, D = (torch.randn((2000, 7000), device="cuda") for _ in range(3))
+    with pytest.raises(ec.EcgemmError) as err:      # (too deep for one launch)
+        own.sgemm_adapters(ec.OP_T, ec.OP_N, 2000, 2000, 7000, 1.0, W, 7000, x, 7000, 2, _offsets([1000, 1000]), _offsets([1]).int(), 1, 8, ec.OP_T, D,
+                           7000, 0, ec.OP_T, D, 8, 0, None, H, 8, 0.0, C, 2000, ec.MODE_FP16_SPLIT)
+    assert err.value.status == ec.ERR_ALLOC
+    torch.cuda.synchronize()
+    assert bool((H == 7.0).all()) and bool((C == 7.0).all())
+    own.destroy()
+
+
+def test_an_infinite_alpha_does_not_meet_what_is_not_there(handle):
+    """No depth: C <- beta C, whatever alpha is."""
+    import torch
+    ec = _ec()
+    for N, M in ((20, 30), (600, 300)):
+        C = Field(M, N, fill=7.0, values=torch.randn((1, N, M), device="cuda"))
+        want = C.view() * 0.5
+        handle.sgemm_grouped(ec.OP_T, ec.OP_N, 1, M, N, 0, float("inf"), None, 0, 0, None, 0, _offsets([N]), 0.5, C.ptr(), C.ld, ec.MODE_FP16_SPLIT)
+        torch.cuda.synchronize()
+        assert torch.equal(C.view(), want)
+    X, G, C = Field(30, 5), Field(20, 5), Field(30, 20, count=2, fill=7.0, values=torch.randn((2, 20, 30), device="cuda"))
+    want = C.view()[1] * 0.5
+    handle.sgemm_grouped_depth(ec.OP_N, ec.OP_T, 2, 30, 20, 5, float("inf"), X.ptr(), X.ld, G.ptr(), G.ld, _offsets([5, 0]), 0.5, C.ptr(), C.ld,
+                               C.stride, ec.MODE_BF16_FULL)
+    torch.cuda.synchronize()
+    assert torch.equal(C.view()[1], want)
