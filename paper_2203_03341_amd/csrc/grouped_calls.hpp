@@ -85,7 +85,7 @@ ecgemm_status_t launch_grouped(ecgemm_handle_t h, ecgemm_mode_t mode, bool depth
 }
 
 // The kernels for few columns to a group (narrow_kernel.hpp).
-constexpr int64_t kAdapterDownMeanColumns = 8, kNarrowProjectionColumns = 96;
+constexpr int64_t kAdapterDownMeanColumns = 8, kNarrowProjectionColumns = 64;
 constexpr int64_t kNarrowTallBlocks = 256;
 constexpr int64_t kAdapterOneLaunchDepth = 6144, kAdapterOneLaunchChunks = 8, kAdapterOneLaunchTiles = 128;
 
@@ -109,6 +109,19 @@ bool narrow_is_faster(bool depth_a, int64_t groups, int64_t M, int64_t N, int64_
   const double tiles_us = 6.0 + std::max(rounds * chunks, bytes / 4.1e6) + (slices > 1 ? 7.0 : 0.0);
   const double pass_us = std::max(bytes / 4.7e6, K / 1024.0 * (depth_a ? 2.9 : 9.3));
   return 4.0 + std::ceil(columns / kNarrowColumns) * pass_us < tiles_us;
+}
+
+// The same for a projection of few columns with adapters, by a pass over A for every 32 columns, and for what ecgemm_sgemm
+// takes with 9 us for the adapters written before.  Calls narrow / the other way, us, A with the depth contiguous, 97 requests of
+// a column, rank 16: 4096 x 4096 70 / 52, 1024 x 2048 39 / 30, 8192 x 2048 68 / 51; 64 of them narrow 44, 25, 41, 65 the other way
+// 53, 30, 50.
+bool narrow_projection_is_faster(bool depth_a, int64_t M, int64_t N, int64_t K, ecgemm_mode_t mode) {
+  if (N > kNarrowProjectionColumns) return false;
+  const Plan pl = make_plan(M, N, K, mode, ECGEMM_SHAPE_AUTO, kOneLaunchSliced);
+  if (pl.shape == nullptr) return true;
+  const double other_us = 9.0 + (pl.shape->fused ? one_launch_us(pl, K, mode) : split_first_us(pl, M, N, K, mode));
+  const double pass_us = std::max(4.0 * M * K / 4.7e6, K / 1024.0 * (depth_a ? 2.9 : 9.3));
+  return 4.0 + std::ceil((double)N / kNarrowColumns) * pass_us < other_us;
 }
 
 // Blocks of 16 rows the operand that is read once is taken in: four where its rows are contiguous, else two where that leaves
@@ -325,7 +338,7 @@ ecgemm_status_t ecgemm_sgemm_adapters(ecgemm_handle_t handle, ecgemm_op_t transA
     if (M == 0) return ECGEMM_OK;
     return sgemm_common(h, transA, transB, M, N, K, alpha, A, lda, B, ldb, beta, C, ldc, mode, nullptr, nullptr, kWorkspaceOfHandle);
   }
-  const bool narrow = project && N <= kNarrowProjectionColumns && lda <= kGroupedLargestLd;
+  const bool narrow = project && lda <= kGroupedLargestLd && narrow_projection_is_faster(transA == ECGEMM_OP_T, M, N, K, mode);
   // Projection and adapters in one launch, where both matrices and H are laid out alike (see grouped_kernel), there are tiles
   // enough for half the chip, no more than a few adapters meet in a tile, and the projection is not so deep that splitting
   // first outweighs two passes over C.  Whole calls so / with C written first and the projection added, us, FP16, M x N x K,
@@ -337,6 +350,8 @@ ecgemm_status_t ecgemm_sgemm_adapters(ecgemm_handle_t handle, ecgemm_op_t transA
   const bool one_launch = project && !narrow && transA == transU && depth_b && groups <= kGroupsPerLaunch && lda <= kGroupedLargestLd &&
                           h->log2_scale_a == 0 && h->log2_scale_b == 0 && K <= kAdapterOneLaunchDepth && tiles >= kAdapterOneLaunchTiles && added_chunks <= kAdapterOneLaunchChunks &&
                           std::fabs(alpha) >= 0x1p-16f && std::fabs(alpha) <= 0x1p16f;  // (H is multiplied by scales / alpha)
+  const int64_t up_columns = N < 2 * kAdapterUpColumnsShort * groups ? kAdapterUpColumnsShort : kAdapterUpColumns;
+  ECGEMM_ARG(h, (M + 255) / 256 * ((N + up_columns - 1) / up_columns) > INT_MAX, 4, "ecgemm_sgemm_adapters: M x N too large");
   if (project && !narrow && !one_launch) {  // what the projection would refuse is refused before anything is enqueued
     st = check_sizes(h, M, N, K, mode, 4);
     if (st != ECGEMM_OK) return st;
@@ -378,7 +393,7 @@ ecgemm_status_t ecgemm_sgemm_adapters(ecgemm_handle_t handle, ecgemm_op_t transA
   }
   if (M == 0) return ECGEMM_OK;
   if (narrow) {
-    // few columns: the projection reads its matrix once, and adds the adapters to what it writes
+    // the projection reads its matrix once (and once more for every 32 columns), and adds the adapters to what it writes
     NarrowParams np{};
     np.A = A, np.lda = lda;
     np.B = B, np.ldb = ldb;
@@ -423,9 +438,15 @@ ecgemm_status_t ecgemm_sgemm_adapters(ecgemm_handle_t handle, ecgemm_op_t transA
   up.index = index, up.matrices = (int)adapters;
   up.scales = scales, up.beta = beta;
   up.row_blocks = (int)((M + 255) / 256);
-  hipLaunchKernelGGL((transU == ECGEMM_OP_T ? adapter_up_kernel<true> : adapter_up_kernel<false>),
-                     dim3((unsigned)(up.row_blocks * ((N + kAdapterUpColumns - 1) / kAdapterUpColumns))), dim3(256), 0, h->stream, up);
-  ECGEMM_HIP(h, hipGetLastError());
+  // Few columns to a request: a block's runs follow each other at 2 us each.  Calls with 64 / 8 columns a block, 128 requests of
+  // a column, rank 16: 4096 x 4096 170 us / 53, 1024 x 2048 150 / 30; 512 of a column, 8192 x 2048, 198 / 108.
+  const bool few = up_columns == kAdapterUpColumnsShort;
+  void (*const up_kernel)(AdapterUpParams) =
+      transU == ECGEMM_OP_T ? (few ? adapter_up_kernel<true, kAdapterUpColumnsShort> : adapter_up_kernel<true, kAdapterUpColumns>)
+                            : (few ? adapter_up_kernel<false, kAdapterUpColumnsShort> : adapter_up_kernel<false, kAdapterUpColumns>);
+  void* up_args[] = {&up};
+  ECGEMM_HIP(h, hipLaunchKernel(reinterpret_cast<const void*>(up_kernel), dim3((unsigned)(up.row_blocks * ((N + up_columns - 1) / up_columns))), dim3(256), up_args,
+                                0, h->stream));
   if (!project) return ECGEMM_OK;
   return sgemm_common(h, transA, transB, M, N, K, alpha, A, lda, B, ldb, 1.0f, C, ldc, mode, nullptr, nullptr, kWorkspaceOfHandle);
 }

@@ -167,8 +167,10 @@ ECGEMM_NARROW_GROUP template __global__ void adapter_down_kernel<true, false, 1>
 ECGEMM_NARROW_GROUP template __global__ void adapter_down_kernel<true, true, 1>(const AdapterDownParams);
 ECGEMM_NARROW_GROUP template __global__ void adapter_down_kernel<true, false, 2>(const AdapterDownParams);
 ECGEMM_NARROW_GROUP template __global__ void adapter_down_kernel<true, true, 2>(const AdapterDownParams);
-ECGEMM_NARROW_GROUP template __global__ void adapter_up_kernel<false>(const AdapterUpParams);
-ECGEMM_NARROW_GROUP template __global__ void adapter_up_kernel<true>(const AdapterUpParams);
+ECGEMM_NARROW_GROUP template __global__ void adapter_up_kernel<false, kAdapterUpColumns>(const AdapterUpParams);
+ECGEMM_NARROW_GROUP template __global__ void adapter_up_kernel<false, kAdapterUpColumnsShort>(const AdapterUpParams);
+ECGEMM_NARROW_GROUP template __global__ void adapter_up_kernel<true, kAdapterUpColumns>(const AdapterUpParams);
+ECGEMM_NARROW_GROUP template __global__ void adapter_up_kernel<true, kAdapterUpColumnsShort>(const AdapterUpParams);
 
 #define ECGEMM_SPLIT_KERNELS_OF(KIND)                                                                     \
   ECGEMM_SPLIT_GROUP template __global__ void split_kernel<KIND, kSplitKContiguous, false>(const SplitJob);      \

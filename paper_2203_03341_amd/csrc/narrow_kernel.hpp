@@ -53,8 +53,8 @@ struct WaveProduct {
   __device__ __forceinline__ int loaded_row(int j) const { return AT_ONCE * j + lane / LANES; }
   __device__ __forceinline__ static int clamped(int i, int count) { return i < count ? i : count - 1; }
 
-  // the stretch from k0 on (the same for the wave), which lies inside the depth; rows contiguous: all 64 rows exist.  Buffer
-  // loads: a scalar base, an offset per lane that never changes, and a scalar offset per load.
+  // the stretch from k0 on (the same for the wave), which lies inside the depth; rows or columns contiguous: as many as whole
+  // loads take (a lane whose own do not exist reads the last ones that do).  Buffer loads: a scalar base, an offset per lane that never changes, and a scalar offset per load.
   __device__ __forceinline__ void fetch(Values& x, int64_t k0) const {
     const auto from_s = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(s + (S_DEPTH ? k0 : k0 * lds)), 0, -1, 0x00020000);
     const auto from_t = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(t + (T_DEPTH ? k0 : k0 * ldt)), 0, -1, 0x00020000);
@@ -67,9 +67,10 @@ struct WaveProduct {
         for (int e = 0; e < 4; ++e) x.s[j][0][e] = v[e];
       }
     } else {
+      const int first = 4 * (lane & 15), at = (int)(((first < rows ? first : rows - 4) + quad * lds) * 4);
 #pragma unroll
       for (int i = 0; i < 4 * QUADS; ++i) {
-        const source4_t v = __builtin_bit_cast(source4_t, __builtin_amdgcn_raw_buffer_load_b128(from_s, (int)((4 * (lane & 15) + quad * lds) * 4), (16 * (i / 4) + i % 4) * s_step, 0));
+        const source4_t v = __builtin_bit_cast(source4_t, __builtin_amdgcn_raw_buffer_load_b128(from_s, at, (16 * (i / 4) + i % 4) * s_step, 0));
 #pragma unroll
         for (int f = 0; f < FR; ++f) x.s[f][i / 4][i % 4] = v[f];
       }
@@ -82,7 +83,6 @@ struct WaveProduct {
         for (int e = 0; e < 4; ++e) x.t[j][0][e] = v[e];
       }
     } else {
-      // (the last lanes' columns do not exist where cols < 16 NF: they read the last ones that do)
       const int first = NF * (lane & 15), at = (int)(((first < cols ? first : cols - NF) + quad * ldt) * 4);
 #pragma unroll
       for (int i = 0; i < 4 * QUADS; ++i) {
@@ -159,7 +159,7 @@ struct WaveProduct {
   // where it begins, going on from the front when it comes to the end: blocks that start together would otherwise all read
   // the same columns of rows that lie a power of two apart, from a few of the memory's channels.
   __device__ __forceinline__ void run(narrow_acc_t (&acc)[FR][NF], int64_t first, int64_t step, unsigned turn) const {
-    const bool vectors = (S_DEPTH || rows >= 64) && (T_DEPTH || cols % NF == 0);
+    const bool vectors = (S_DEPTH || rows % 4 == 0) && (T_DEPTH || cols % NF == 0);
     const int64_t whole = vectors ? K / STRETCH : 0, all = (K + STRETCH - 1) / STRETCH;
     const int64_t begin = (int64_t)(((uint64_t)turn * (uint64_t)whole) >> 32);
     auto k_at = [&](int64_t stretch) {
@@ -327,7 +327,10 @@ __global__ void __launch_bounds__(kNarrowThreads, DEPTH_A && FR == 1 ? 4 : 2) na
   const float* a = p.A + matrix * p.stride_a + (DEPTH_A ? m0 * p.lda : m0);
   for (int64_t n0 = begin; n0 < end; n0 += kNarrowColumns) {
     const int cols = (int)(end - n0 < kNarrowColumns ? end - n0 : kNarrowColumns);
-    if (p.U != nullptr) find_adapters(p.adapter_offsets, p.adapter_groups, p.index, p.matrices, p.N, n0, cols, adapter, kNarrowThreads);
+    if (p.U != nullptr) {
+      __syncthreads();  // the adapters of the columns before are no longer looked at
+      find_adapters(p.adapter_offsets, p.adapter_groups, p.index, p.matrices, p.N, n0, cols, adapter, kNarrowThreads);
+    }
     narrow_block<DEPTH_A, DEPTH_B, FR, false>(a, p.lda, rows, p.B + (DEPTH_B ? n0 * p.ldb : n0), p.ldb, cols, matrix >= 0 ? p.K : 0, sums);
     for (int i = threadIdx.x; i < ROWS * cols; i += kNarrowThreads) {
       const int r = i % ROWS, c = i / ROWS;
@@ -406,9 +409,10 @@ __global__ void __launch_bounds__(kNarrowThreads, 2) adapter_down_kernel(const A
   }
 }
 
-constexpr int kAdapterUpColumns = 64;
+constexpr int kAdapterUpColumns = 64, kAdapterUpColumnsShort = 8;
 // The second half: C = scales[a] op(U_a) H + beta C in every column, before the projection is added.  A block takes 256 rows
-// of C and 64 columns, a wave 64 rows, run by run of columns with the same adapter; the depth is the rank.  Bound by writing C (and by reading it, unless beta is zero).
+// of C and 64 columns (8 where there are few to a request), a wave 64 rows, run by run of columns with the same adapter; the
+// depth is the rank.  Bound by writing C (and by reading it, unless beta is zero).
 struct AdapterUpParams {
   const float* U;
   const float* H;
@@ -422,19 +426,19 @@ struct AdapterUpParams {
   float* C;
   int row_blocks;
 };
-template <bool DEPTH_U>
+template <bool DEPTH_U, int COLUMNS>
 __global__ void __launch_bounds__(256) adapter_up_kernel(const AdapterUpParams p) {
-  __shared__ int adapter[kAdapterUpColumns / kNarrowColumns][kNarrowColumns];
+  __shared__ int adapter[(COLUMNS + kNarrowColumns - 1) / kNarrowColumns][kNarrowColumns];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t n0 = (int64_t)(blockIdx.x / (unsigned)p.row_blocks) * kAdapterUpColumns;
+  const int64_t n0 = (int64_t)(blockIdx.x / (unsigned)p.row_blocks) * COLUMNS;
   const int64_t m0 = (int64_t)(blockIdx.x % (unsigned)p.row_blocks) * 256 + 64 * wave;
-  const int cols = (int)(p.N - n0 < kAdapterUpColumns ? p.N - n0 : kAdapterUpColumns);
-  for (int i = 0; i < kAdapterUpColumns / kNarrowColumns; ++i)
+  const int cols = (int)(p.N - n0 < COLUMNS ? p.N - n0 : COLUMNS);
+  for (int i = 0; i * kNarrowColumns < cols; ++i)
     find_adapters(p.offsets, p.groups, p.index, p.matrices, p.N, n0 + i * kNarrowColumns, kNarrowColumns, adapter[i], 256);
   if (m0 >= p.M) return;
   const int rows = (int)(p.M - m0 < 64 ? p.M - m0 : 64);
   auto adapter_of = [&](int c) { return uniform(adapter[c / kNarrowColumns][c % kNarrowColumns]); };
-  constexpr int NF = kAdapterUpColumns / 16;
+  constexpr int NF = (COLUMNS + 15) / 16;
   typedef WaveProduct<DEPTH_U, true, 4, NF> Product;
   __shared__ __attribute__((aligned(16))) float space[4][Product::SPACE];
   for (int first = 0; first < cols;) {

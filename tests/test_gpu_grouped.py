@@ -743,3 +743,19 @@ def test_an_infinite_alpha_does_not_meet_what_is_not_there(handle):
                                C.stride, ec.MODE_BF16_FULL)
     torch.cuda.synchronize()
     assert torch.equal(C.view()[1], want)
+
+
+@pytest.mark.parametrize("trans", ["NNNN", "TNTT", "TNTN", "NTNT", "TTTT"])
+def test_adapters_of_single_tokens_in_more_than_one_pass(handle, trans):
+    """Decoding steps of more requests than a pass of the narrow kernel holds, in the storage orders of forward and backward: the
+    adapters of a pass must not be those of the next one."""
+    rng = np.random.RandomState(31)
+    for M, K, N, R in ((1826, 3000, 40, 48), (300, 900, 64, 16), (258, 700, 130, 12)):
+        for mode in MODES:
+            _run_adapters(handle, mode, M, N, K, R, [1] * (N - 3), list(rng.randint(-1, 5, N - 3)), 5, trans=trans, start=1, seed=N)
+
+
+@pytest.mark.parametrize("M", [4, 8, 12, 48, 60, 62, 64, 68, 100])
+def test_few_columns_with_contiguous_rows_of_every_number(handle, M):
+    for trans in ("NN", "NT"):
+        _run_columns(handle, trans, "fp16", M, 200, [1, 3, 17, 33, 2], start=1, behind=1, pad=(1, 0, 2), seed=M)
