@@ -6,7 +6,7 @@
 // v_mfma_f32_16x16x4_f32, 16 rows and 16 columns, four of the depth.  The result is at least as exact as either mode's,
 // values far from 1, infinities and NaN included.  What is arranged is the traffic:
 //   * a block takes 16 rows (64 where rows are contiguous) and all the group's columns, its eight waves share the depth
-//     between them, each taking every eighth stretch, so that the block reads runs of 2 KiB of every row; the eight sums
+//     between them, each taking every eighth stretch, so that the block reads runs of 1 KiB of every row; the eight sums
 //     meet in LDS and are added in order.
 //   * an instruction takes row and column l % 16 from lane l.  Loads in that order have neighbouring lanes in different rows,
 //     and the memory path takes 16 bytes a cycle then instead of 64 (4096 x 4096 times 32 columns 27 us, three quarters of
@@ -14,6 +14,8 @@
 //     of LDS that is the wave's own.
 //   * lane l's float4 at 4 (l / 16) of a quad of 16 k is its part of four instructions, for either operand.
 //   * two stretches are in flight in registers while a third one is multiplied.
+// Measured: 64 groups of 2 columns, 1536 x 2048 each, 130 us, 6.2 TB/s; one of 4096 x 4096 13.3 us with up to 16 columns, 16.0
+// with 32; eight of 768 x 1024 with 16 columns together 6.8.
 #pragma once
 #include "grouped_kernel.hpp"
 
