@@ -86,7 +86,7 @@ ecgemm_status_t launch_grouped(ecgemm_handle_t h, ecgemm_mode_t mode, bool depth
 
 // The kernels for few columns to a group (narrow_kernel.hpp).
 constexpr int64_t kAdapterDownMeanColumns = 8, kNarrowProjectionColumns = 64;
-constexpr int64_t kNarrowTallBlocks = 256;
+constexpr int64_t kNarrowTallBlocks = 256, kShallowMeanDepth = 16, kShallowMeanDepthSlim = 64;
 constexpr int64_t kAdapterOneLaunchDepth = 6144, kAdapterOneLaunchChunks = 8, kAdapterOneLaunchTiles = 128;
 
 // Whether ecgemm_sgemm_grouped runs on narrow_kernel, by what either kernel is estimated to take (us), all groups taken as
@@ -254,6 +254,28 @@ ecgemm_status_t ecgemm_sgemm_grouped_depth(ecgemm_handle_t handle, ecgemm_op_t t
   }
   const OnDeviceOf device(h);
   if (device.error != hipSuccess) return hip_fail(h, device.error, "hipSetDevice");
+  const int64_t row_blocks = (M + 255) / 256, column_blocks = (N + kShallowColumns - 1) / kShallowColumns;
+  // Shallow groups, by their mean depth.  Tiles / shallow, us, FP16, groups of M x N: 64 of 1024 x 768, of depth 1 66 / 58, 16 66 /
+  // 55, 32 66 / 63 and 97 / 112 with beta; 51 of 1792 x 1216, 1 146 / 110, 16 146 / 119, 32 146 / 158; 4 of 4096 x 4096, 1 86 / 60, 32 87 /
+  // 77, 48 87 / 99; 11 of 320 x 1664, 16 16 / 13.6, 32 with beta 20 / 28.  One side of 64 or less, which a tile only half fills: 8 of
+  // 64 x 4096, 1 10.1 / 5.9, 64 9.6 / 7.8, 128 10.3 / 11.7; 4096 x 64 alike.
+  const int64_t shallow = M <= 64 || N <= 64 ? kShallowMeanDepthSlim : kShallowMeanDepth;
+  if (K <= shallow * groups && row_blocks * column_blocks <= INT_MAX / groups) {
+    ShallowParams sp{};
+    sp.A = A, sp.lda = lda;
+    sp.B = B, sp.ldb = ldb;
+    sp.C = C, sp.ldc = ldc, sp.stride_c = strideC;
+    sp.M = M, sp.N = N, sp.K = K;
+    sp.offsets = offsets;
+    sp.alpha = alpha, sp.beta = beta;
+    sp.row_blocks = (int)row_blocks, sp.column_blocks = (int)column_blocks;
+    static void (*const kernels[2][2])(ShallowParams) = {{shallow_kernel<false, false>, shallow_kernel<false, true>},
+                                                         {shallow_kernel<true, false>, shallow_kernel<true, true>}};
+    void* args[] = {&sp};
+    ECGEMM_HIP(h, hipLaunchKernel(reinterpret_cast<const void*>(kernels[transA == ECGEMM_OP_T][transB == ECGEMM_OP_N]),
+                                  dim3((unsigned)(groups * row_blocks * column_blocks)), dim3(256), args, 0, h->stream));
+    return ECGEMM_OK;
+  }
   GroupedParams gp{};
   gp.A = A, gp.lda = lda;
   gp.B = B, gp.ldb = ldb;

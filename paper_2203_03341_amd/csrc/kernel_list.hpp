@@ -172,6 +172,11 @@ ECGEMM_NARROW_GROUP template __global__ void adapter_up_kernel<false, kAdapterUp
 ECGEMM_NARROW_GROUP template __global__ void adapter_up_kernel<true, kAdapterUpColumns>(const AdapterUpParams);
 ECGEMM_NARROW_GROUP template __global__ void adapter_up_kernel<true, kAdapterUpColumnsShort>(const AdapterUpParams);
 
+ECGEMM_NARROW_GROUP template __global__ void shallow_kernel<false, false>(const ShallowParams);
+ECGEMM_NARROW_GROUP template __global__ void shallow_kernel<false, true>(const ShallowParams);
+ECGEMM_NARROW_GROUP template __global__ void shallow_kernel<true, false>(const ShallowParams);
+ECGEMM_NARROW_GROUP template __global__ void shallow_kernel<true, true>(const ShallowParams);
+
 #define ECGEMM_SPLIT_KERNELS_OF(KIND)                                                                     \
   ECGEMM_SPLIT_GROUP template __global__ void split_kernel<KIND, kSplitKContiguous, false>(const SplitJob);      \
   ECGEMM_SPLIT_GROUP template __global__ void split_kernel<KIND, kSplitRContiguous, false>(const SplitJob);      \

@@ -759,3 +759,14 @@ def test_adapters_of_single_tokens_in_more_than_one_pass(handle, trans):
 def test_few_columns_with_contiguous_rows_of_every_number(handle, M):
     for trans in ("NN", "NT"):
         _run_columns(handle, trans, "fp16", M, 200, [1, 3, 17, 33, 2], start=1, behind=1, pad=(1, 0, 2), seed=M)
+
+
+@pytest.mark.parametrize("trans", ["NT", "NN", "TT", "TN"])
+def test_shallow_groups_of_the_depth(handle, trans):
+    """Groups a few deep, few and many rows and columns, each way of adding to C; and as deep as one of them happens to be."""
+    for mode in MODES:
+        _run_depth(handle, trans, mode, 260, 130, [1, 0, 2, 16, 17, 3, 5, 0], start=2, behind=3, pad=(1, 2, 3))
+        _run_depth(handle, trans, mode, 256, 128, [1, 4, 33, 0, 0, 0, 1, 1], alpha=1.5, beta=-0.5)
+        _run_depth(handle, trans, mode, 7, 300, [40, 100, 0], alpha=-1.0, beta=1.0, pad=(2, 0, 1))
+        _run_depth(handle, trans, mode, 300, 5, [64, 20, 9], pad=(0, 1, 0))
+        _run_depth(handle, trans, mode, 64, 64, [1] * 70)
