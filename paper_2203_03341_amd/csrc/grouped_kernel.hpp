@@ -102,7 +102,11 @@ struct GroupedOperand {
   int64_t ld, K;
   int row, octet;      // of this thread's unit 0
   int rows;            // DEPTH: rows that exist; else: rows in memory
-  bool straddles;      // !DEPTH, the same for the block: the last rows in memory are fewer than a load takes
+  // !DEPTH, the same for the block: the last rows in memory are fewer than a load takes, so that lane reads the last ones that
+  // fill one, `shift` rows earlier, and realign() moves them; or all of them are, and they are read one by one.  (Every tile
+  // that straddles with its rows read one by one: eight gradients of 1001 x 2003 over 8192 262 us instead of 134.)
+  bool straddles, tiny;
+  int shift;
   unsigned lane_bytes[DEPTH ? UNITS : 1];
   float factor;
 
@@ -134,18 +138,19 @@ struct GroupedOperand {
     octet = DEPTH ? t % OCTETS : t / (kGroupedTile / UNITS);
     row = DEPTH ? t / OCTETS : UNITS * (t % (kGroupedTile / UNITS));
     rows = DEPTH ? exist : readable;
-    straddles = !DEPTH && readable < kGroupedTile && readable % UNITS != 0;
+    tiny = !DEPTH && readable < UNITS;
+    straddles = !DEPTH && !tiny && readable < kGroupedTile && readable % UNITS != 0;
     if constexpr (DEPTH) {
 #pragma unroll
       for (int u = 0; u < UNITS; ++u) lane_bytes[u] = (unsigned)((clamped_row(u) * ld + 8 * octet) * 4);
     } else {
-      // (not used where the rows straddle)
       const int start = row + UNITS <= rows ? row : rows >= UNITS ? rows - UNITS : 0;
       lane_bytes[0] = (unsigned)((8 * octet * ld + start) * 4);
+      shift = row - start;
     }
   }
 
-  // Loads FIRST .. FIRST + COUNT - 1 of chunk c, which lies inside the depth; rows do not straddle.
+  // Loads FIRST .. FIRST + COUNT - 1 of chunk c, which lies inside the depth; not tiny.
   static constexpr int LOADS = DEPTH ? 2 * UNITS : 8;
   template <int FIRST = 0, int COUNT = LOADS>
   __device__ __forceinline__ void fetch(float (&x)[VALUES], int c) const {
@@ -187,7 +192,7 @@ struct GroupedOperand {
         for (int i = 0; i < VALUES; ++i) x[i] = load_global(first + clamped_row(i >> 3) * ld + (k0 + (i & 7) < K ? k0 + (i & 7) : K - 1));
       }
     } else {
-      if (!straddles) {
+      if (!tiny) {
         const int start = row + UNITS <= rows ? row : rows - UNITS;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -216,6 +221,19 @@ struct GroupedOperand {
     } else {
 #pragma unroll
       for (int i = 0; i < VALUES; ++i) x[i] = k0 + (i & 7) < K ? x[i] : 0.0f;
+    }
+  }
+
+  // The rows of a lane that read earlier ones, in their places (rows that do not exist hold anything)
+  __device__ __forceinline__ void realign(float (&x)[VALUES]) const {
+    if constexpr (!DEPTH) {
+      if (!straddles) return;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+          for (int d = 1; u + d < UNITS; ++d) x[8 * u + j] = shift == d ? x[8 * (u + d) + j] : x[8 * u + j];
     }
   }
 
@@ -520,6 +538,7 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_kernel(const Group
         char* stage = lds + (number & 1) * STAGE_BYTES;
         oa.fetch_any(va, c);
         oa.complete(va, c);
+        oa.realign(va);
         if constexpr (careful) oa.deposit_with_care(va, stage);
         else oa.template deposit<false, false, 0>(va, stage, 0);
         __builtin_amdgcn_sched_barrier(0);
@@ -545,7 +564,8 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_kernel(const Group
       float xa[2][VALUES], xb[2][VALUES];
       a.init(it.a, p.lda, it.K, it.rows, it.readable_rows, p.prescale_a, t);
       b.init(it.b, p.ldb, it.K, it.cols, it.readable_cols, p.prescale_b, t);
-      const int whole = a.straddles || b.straddles ? 0 : (int)(it.K / CHUNK);
+      const int whole = a.tiny || b.tiny ? 0 : (int)(it.K / CHUNK);
+      const int bulk = a.straddles || b.straddles ? 0 : whole;  // (the loop of whole chunks has no rows to move)
       auto request = [&](auto r_c, int c) {
         constexpr int r = decltype(r_c)::value;
         if (c < whole) a.fetch(xa[r], c), b.fetch(xb[r], c);
@@ -563,8 +583,8 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_kernel(const Group
       int c = 0;
       // the bulk of the depth: chunks that lie inside it, and so do those requested behind them
       typename OperandA::uint4_t ahead[NP];
-      if (c + 4 <= whole) a.template convert<SCALED>(xa[0], 0, ahead);
-      for (; c + 4 <= whole; c += 2) {
+      if (c + 4 <= bulk) a.template convert<SCALED>(xa[0], 0, ahead);
+      for (; c + 4 <= bulk; c += 2) {
         static_for<2>([&](auto r_c) {
           constexpr int r = decltype(r_c)::value;
           a.write(ahead, 0, lds + r * STAGE_BYTES);
@@ -579,6 +599,7 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_kernel(const Group
           constexpr int r = decltype(r_c)::value;
           if (c + r < chunks) {
             if (c + r >= whole) a.complete(xa[r], c + r), b.complete(xb[r], c + r);
+            a.realign(xa[r]), b.realign(xb[r]);
             a.template deposit<SCALED, false, 0>(xa[r], lds + r * STAGE_BYTES, 0);
             b.template deposit<SCALED, false, 0>(xb[r], lds + r * STAGE_BYTES + REGION_BYTES, 0);
             __builtin_amdgcn_sched_barrier(0);
@@ -607,6 +628,7 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_kernel(const Group
           char* stage = lds + (c & 1) * STAGE_BYTES;
           a.fetch_any(xa, c), b.fetch_any(xb, c);
           a.complete(xa, c), b.complete(xb, c);
+          a.realign(xa), b.realign(xb);
           a.deposit_with_care(xa, stage);
           b.deposit_with_care(xb, stage + REGION_BYTES);
           block_barrier();

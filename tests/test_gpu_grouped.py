@@ -770,3 +770,36 @@ def test_shallow_groups_of_the_depth(handle, trans):
         _run_depth(handle, trans, mode, 7, 300, [40, 100, 0], alpha=-1.0, beta=1.0, pad=(2, 0, 1))
         _run_depth(handle, trans, mode, 300, 5, [64, 20, 9], pad=(0, 1, 0))
         _run_depth(handle, trans, mode, 64, 64, [1] * 70)
+
+
+@pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("M", [33, 34, 35, 61, 129, 130, 131, 133, 254, 255, 257, 387])
+def test_contiguous_rows_of_every_remainder(handle, M, mode):
+    """The last rows of a tile are fewer than a load takes: they come with earlier ones, and none is written twice or skipped."""
+    _run_columns(handle, "NT", mode, M, 333, [1, 7, 30, 2], alpha=1.5, beta=-0.5, pad=(1, 0, 2), seed=M)
+    _run_columns(handle, "NN", mode, M, 520, [150, 129, 200], start=1, behind=2, alpha=1.5, beta=-0.5, pad=(0, 1, 0), seed=M)
+    _run_columns(handle, "NT", mode, M, 65, [M, 129, 0, 200], pad=(2, 3, 0), seed=M)
+    _run_depth(handle, "NT", mode, M, M + 1, [500, 129, 64, 0, 321], alpha=1.5, beta=1.0, pad=(1, 1, 1), seed=M)
+    _run_adapters(handle, mode, M, 24, 200, 8, [3, 9, 12], [1, 0, 1], 2, trans="NNNN", beta=0.5)
+    _run_adapters(handle, mode, M, 300, 200, 8, [100, 41, 159], [1, 0, 1], 2, trans="NNNN", beta=0.5)
+
+
+@pytest.mark.parametrize("mode", MODES)
+def test_values_that_are_not_finite_in_the_last_contiguous_rows(handle, mode):
+    import torch
+    ec = _ec()
+    for M, N, K in [(131, 200, 192), (131, 12, 192), (387, 300, 65), (61, 20, 64)]:
+        A, B = torch.randn((K, M), device="cuda"), torch.randn((N, K), device="cuda")
+        A[K // 2, M - 1] = float("inf")
+        B[3, 5] = float("nan")
+        C = torch.full((N, M), 7.0, device="cuda")
+        handle.sgemm_grouped(ec.OP_N, ec.OP_N, 1, M, N, K, 1.0, A.data_ptr(), M, 0, B.data_ptr(), K, _offsets([N]), 0.0, C.data_ptr(), M,
+                             _mode(mode))
+        exact = (B.double().cpu() @ A.double().cpu()).cuda()
+        mask = exact.isfinite()
+        assert torch.equal(C.isfinite(), mask)      # (an infinity may come out as a NaN: its parts meet others of either sign)
+        a, b = A.clone(), B.clone()
+        a[K // 2, M - 1] = 0.0
+        b[3, 5] = 0.0
+        allowed = _allowed(a.t().double(), b.t().double(), mode, 1.0, 0.0, None).t()
+        assert bool(((C.double() - exact).abs()[mask] <= allowed[mask]).all())
