@@ -803,3 +803,39 @@ def test_values_that_are_not_finite_in_the_last_contiguous_rows(handle, mode):
         b[3, 5] = 0.0
         allowed = _allowed(a.t().double(), b.t().double(), mode, 1.0, 0.0, None).t()
         assert bool(((C.double() - exact).abs()[mask] <= allowed[mask]).all())
+
+
+@pytest.mark.parametrize("M", [2001, 2050, 2051])
+def test_adapters_in_tiles_with_contiguous_rows_of_every_remainder(handle, M):
+    _run_adapters(handle, "fp16", M, 1100, 150, 20, [500, 1, 599], [1, 0, 1], 2, trans="NNNN", beta=0.5, pad=1)
+    _run_adapters(handle, "bf16", M, 1100, 150, 20, [500, 1, 599], [1, 0, 1], 2, trans="NNTN", pad=1)
+
+
+@pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("trans", ["NT", "NN", "TT", "TN"])
+def test_shallow_groups_keep_to_themselves(handle, trans, mode):
+    """What is not finite in one group's tokens reaches that group's C only, and there the row or column it belongs to."""
+    import torch
+    gen, M, N, sizes = _gen(3), 200, 140, [3, 0, 5, 1, 18, 2]
+    K, starts = sum(sizes), np.concatenate([[0], np.cumsum(sizes)])
+    A = Field(*((M, K) if trans[0] == "N" else (K, M)), gen=gen)
+    B = Field(*((K, N) if trans[1] == "N" else (N, K)), gen=gen)
+    results = []
+    for spoilt in (False, True):
+        a = A.view()[0] if trans[0] == "N" else A.view()[0].t()     # [k, m]
+        b = B.view()[0].t() if trans[1] == "N" else B.view()[0]     # [k, n]
+        if spoilt:
+            a[starts[2] + 1, 7] = float("inf")
+            a[starts[4] + 17, 199] = float("nan")
+            b[starts[2], 139] = -float("inf")
+            b[starts[5], 0] = float("nan")
+        C = Field(M, N, count=len(sizes), gap=3, fill=7.0)
+        handle.sgemm_grouped_depth(_ops(trans[0]), _ops(trans[1]), len(sizes), M, N, K, 1.0, A.ptr(), A.ld, B.ptr(), B.ld, _offsets(sizes),
+                                   0.0, C.ptr(), C.ld, C.stride, _mode(mode))
+        torch.cuda.synchronize()
+        results.append(C.view().clone())     # [g, n, m]
+    clean, spoilt = results
+    touched = torch.zeros_like(clean, dtype=torch.bool)
+    touched[2, :, 7] = touched[2, 139] = touched[4, :, 199] = touched[5, 0] = True
+    assert torch.equal(clean[~touched], spoilt[~touched])
+    assert not bool(torch.isfinite(spoilt[touched]).any())
