@@ -598,7 +598,7 @@ def test_refusals(handle):
                                "scales H ldh beta C ldc mode"}
     sound = dict(transA=ec.OP_T, transB=ec.OP_N, groups=3, M=8, N=8, K=8, alpha=1.0, A=t, lda=8, strideA=64, B=t[1024:], ldb=8, offsets=offs,
                  beta=0.0, C=t[2048:], ldc=8, strideC=64, mode=ec.MODE_FP16_SPLIT, index=index, adapters=2, rank=4, transD=ec.OP_T, D=t, ldd=8,
-                 strideD=32, transU=ec.OP_T, U=t, ldu=4, strideU=32, scales=None, H=t[3072:], ldh=4)
+                 strideD=32, transU=ec.OP_T, U=t, ldu=4, strideU=32, scales=None, H=t[2560:], ldh=4)
     wrong = {name: [dict(transA=2), dict(transB=-1), dict(M=-1), dict(N=-1), dict(K=-1), dict(groups=-1), dict(A=None), dict(lda=7), dict(B=None),
                     dict(ldb=7), dict(C=None), dict(ldc=7), dict(offsets=None), dict(offsets=offs.data_ptr() + 4), dict(mode=11), dict(mode=-1),
                     dict(M=1 << 31), dict(N=1 << 31), dict(K=1 << 31, lda=1 << 31, ldb=1 << 31), dict(groups=1 << 31)] for name in names}
