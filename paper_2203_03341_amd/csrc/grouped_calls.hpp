@@ -29,11 +29,10 @@ grouped_fn_t grouped_kernel_of(bool depth_a, bool depth_b) {
 }
 
 constexpr int64_t kGroupedMostTiles = 1 << 30;
-int64_t tiles_of(int64_t v) { return (v + kGroupedTile - 1) / kGroupedTile; }
 // Most tiles that a call with groups of columns, or all that one with groups of the depth can have in one launch.
 int64_t most_grouped_tiles(bool along_depth, int64_t groups, int64_t M, int64_t N) {
   const int64_t g = std::min<int64_t>(groups, kGroupsPerLaunch);
-  return along_depth ? g * tiles_of(M) * tiles_of(N) : tiles_of(M) * (N / kGroupedTile + std::min(g, N));
+  return along_depth ? g * grouped_tiles(M) * grouped_tiles(N) : grouped_tiles(M) * (N / kGroupedTile + std::min(g, N));
 }
 
 // Slices of the depth: where the tiles are few, as many as fill the chip, 512 deep at least, and only if that saves more than
@@ -50,8 +49,8 @@ ecgemm_status_t launch_grouped(ecgemm_handle_t h, ecgemm_mode_t mode, bool depth
   gp.prescale_a = std::ldexp(1.0f, h->log2_scale_a);
   gp.prescale_b = std::ldexp(1.0f, h->log2_scale_b);
   gp.out_scale = std::ldexp(1.0f, -(h->log2_scale_a + h->log2_scale_b));
-  gp.tiles_m = (int)tiles_of(gp.M);
-  gp.tiles_n = gp.along_depth ? (int)tiles_of(gp.N) : 0;
+  gp.tiles_m = (int)grouped_tiles(gp.M);
+  gp.tiles_n = gp.along_depth ? (int)grouped_tiles(gp.N) : 0;
   const grouped_fn_t kernel = mode == ECGEMM_MODE_FP16_SPLIT
                                   ? (scaled ? grouped_kernel_of<kMethodFp16Split, true>(depth_a, depth_b) : grouped_kernel_of<kMethodFp16Split, false>(depth_a, depth_b))
                                   : (scaled ? grouped_kernel_of<kMethodBf16Full, true>(depth_a, depth_b) : grouped_kernel_of<kMethodBf16Full, false>(depth_a, depth_b));
@@ -103,7 +102,7 @@ constexpr int64_t kAdapterOneLaunchDepth = 6144, kAdapterOneLaunchChunks = 8, kA
 bool narrow_is_faster(bool depth_a, int64_t groups, int64_t M, int64_t N, int64_t K, ecgemm_mode_t mode) {
   const double bytes = 4.0 * groups * M * K, columns = (double)N / groups;
   if (columns > kGroupedTile) return false;  // (not measured)
-  const double rounds = std::ceil((double)tiles_of(M) * groups * std::ceil(columns / kGroupedTile) / kPlanComputeUnits);
+  const double rounds = std::ceil((double)grouped_tiles(M) * groups * std::ceil(columns / kGroupedTile) / kPlanComputeUnits);
   const int slices = grouped_slices(most_grouped_tiles(false, groups, M, N), K);
   const double chunks = (K / 64.0) * (mode == ECGEMM_MODE_FP16_SPLIT ? 0.95 : 1.5) / slices;
   const double tiles_us = 6.0 + std::max(rounds * chunks, bytes / 4.1e6) + (slices > 1 ? 7.0 : 0.0);
@@ -368,7 +367,7 @@ ecgemm_status_t ecgemm_sgemm_adapters(ecgemm_handle_t handle, ecgemm_op_t transA
   // 2048 x 1024, 16, 4 43 / 51, x 512 37 / 33; 2048 x 6000 x 5120, 64, 4 452 / 524; 8192 x 4096 x 8192, 32, 4 1534 / 1480; BF16 4096^3,
   // 16, 4 610 / 665; 2049 x 1040 x 1500, 20, 61 76 / 100.
   const int64_t chunk = mode == ECGEMM_MODE_FP16_SPLIT ? 64 : 32, added_chunks = (1 + kGroupedTile * groups / N) * ((rank + chunk - 1) / chunk);
-  const int64_t tiles = tiles_of(M) * tiles_of(N);
+  const int64_t tiles = grouped_tiles(M) * grouped_tiles(N);
   const bool one_launch = project && !narrow && transA == transU && depth_b && groups <= kGroupsPerLaunch && lda <= kGroupedLargestLd &&
                           h->log2_scale_a == 0 && h->log2_scale_b == 0 && K <= kAdapterOneLaunchDepth && tiles >= kAdapterOneLaunchTiles && added_chunks <= kAdapterOneLaunchChunks &&
                           std::fabs(alpha) >= 0x1p-16f && std::fabs(alpha) <= 0x1p16f;  // (H is multiplied by scales / alpha)
@@ -435,7 +434,7 @@ ecgemm_status_t ecgemm_sgemm_adapters(ecgemm_handle_t handle, ecgemm_op_t transA
     gp.M = M, gp.N = N, gp.K = K;
     gp.offsets = offsets, gp.groups = (int)groups;
     gp.index = index, gp.matrices = (int)adapters, gp.scales = scales;
-    gp.tiles_m = (int)tiles_of(M), gp.tiles_n = (int)tiles_of(N);
+    gp.tiles_m = (int)grouped_tiles(M), gp.tiles_n = (int)grouped_tiles(N);
     gp.U = U, gp.ldu = ldu, gp.stride_u = strideU, gp.rank = rank;
     gp.H = H, gp.ldh = ldh;
     gp.prescale_a = gp.prescale_b = gp.out_scale = 1.0f;

@@ -19,11 +19,12 @@
 // 368 FP32-equivalent TFLOP/s (BF16 598), eight groups of 1024 columns, 4096 x 2048, 400.  60 % of the cycles are matrix
 // instructions, at 1.7 GHz: the board is at its power cap.
 #pragma once
+#include "grouped_sizes.hpp"
 #include "wide_kernel.hpp"
 
 namespace ecgemm {
 
-constexpr int kGroupedTile = 128, kGroupedThreads = 512, kGroupedSplitWaves = 4;
+constexpr int kGroupedThreads = 512, kGroupedSplitWaves = 4;
 constexpr int kGroupsPerLaunch = 1024;             // the table of the groups lies in LDS; more groups are more launches
 constexpr int kGroupedTilesPerBlock = 1024;        // most tiles a block walks through (a byte of LDS per tile and wave)
 constexpr int64_t kGroupedLargestLd = (int64_t)1 << 21;  // a chunk's values lie within 2^30 bytes of its first
@@ -333,7 +334,7 @@ __device__ __forceinline__ void make_group_table(const GroupedParams& p, GroupTa
         adapters->adapter[g] = adapter;
         adapters->scale[g] = adapter >= 0 && p.scales != nullptr ? p.scales[adapter] : 1.0f;
       }
-      tiles[i] = (int)((end - begin + kGroupedTile - 1) / kGroupedTile);
+      tiles[i] = (int)grouped_tiles(end - begin);
     }
     sum += tiles[i];  // (at most 2 x 2^24)
   }
@@ -406,7 +407,7 @@ __device__ __forceinline__ GroupedItem grouped_item(const GroupedParams& p, cons
     group = group < p.groups ? group : p.groups - 1;
     const int begin = uniform(table.begin[group]), end = uniform(table.end[group]);
     const int first_tile = uniform(table.first_tile[group]);
-    const int tiles_n = (end - begin + kGroupedTile - 1) / kGroupedTile;
+    const int tiles_n = (int)grouped_tiles(end - begin);
     const int64_t within = index - (int64_t)first_tile * p.tiles_m;
     // (only offsets that decrease can bring a tile that does not exist: it has no columns and is passed over)
     tile_m = 0, tile_n = tiles_n;

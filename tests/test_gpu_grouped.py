@@ -839,3 +839,24 @@ def test_shallow_groups_keep_to_themselves(handle, trans, mode):
     touched[2, :, 7] = touched[2, 139] = touched[4, :, 199] = touched[5, 0] = True
     assert torch.equal(clean[~touched], spoilt[~touched])
     assert not bool(torch.isfinite(spoilt[touched]).any())
+
+
+def test_one_group_of_the_most_columns_there_can_be(handle):
+    """Rounding its columns up to whole tiles passes 32 bits.  Every element is written, and none before or behind C."""
+    import torch
+    ec, N, guard = _ec(), (1 << 31) - 1, 1024
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 24 GiB of GPU memory")
+    A = torch.full((1,), 2.0, device="cuda")
+    B, C = (torch.full((N + 2 * guard,), v, device="cuda") for v in (1.5, 7.0))
+    ends = {0: 5.0, 1: -1.0, 126: 4.0, 128: 9.0, N // 2: 0.25, N - 128: 6.0, N - 2: 8.0, N - 1: -3.0}
+    for j, v in ends.items():
+        B[guard + j] = v
+    handle.sgemm_grouped(ec.OP_N, ec.OP_N, 1, 1, N, 1, 1.0, A, 1, 1, B[guard:], 1, _offsets([N]), 0.0, C[guard:], 1, ec.MODE_FP16_SPLIT)
+    torch.cuda.synchronize()
+    for j, v in ends.items():       # products of a few bits: exact in either mode
+        assert float(C[guard + j]) == 2.0 * v, j
+        C[guard + j] = 3.0
+    assert bool((C[:guard] == 7.0).all()) and bool((C[guard + N:] == 7.0).all())
+    step = 1 << 28
+    assert all(bool((C[guard + at:min(guard + at + step, guard + N)] == 3.0).all()) for at in range(0, N, step))

@@ -31,3 +31,51 @@ def test_the_header_says_the_same_constants():
     text = open(os.path.join(root, "include", "ecgemm.h")).read()
     mib = int(re.search(r"#define ECGEMM_GROUPED_WORKSPACE_BYTES \(\(size_t\)(\d+) << 20\)", text)[1])
     assert mib << 20 == ec.GROUPED_WORKSPACE_BYTES
+
+
+def _run_on_the_sizes(tmp_path, body):
+    """Compiles `body` as the main function of a program that includes the sizes' header, with the host compiler, and runs it."""
+    import os
+    import shutil
+    import subprocess
+    import pytest
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    if not shutil.which("g++"):
+        pytest.skip("no host compiler")
+    (tmp_path / "sizes.cpp").write_text(
+        '#include "grouped_sizes.hpp"\n#include <cstdio>\n#include <initializer_list>\nusing namespace ecgemm;\n'
+        '#define CHECK(cond) do { if (!(cond)) { std::printf("line %d: %s\\n", __LINE__, #cond); return 1; } } while (0)\n'
+        "int main() {\n" + body + "\nreturn 0;\n}\n")
+    exe = str(tmp_path / "sizes")
+    built = subprocess.run(["g++", "-std=c++17", "-Wall", "-Werror", "-fsanitize=undefined", "-fno-sanitize-recover=undefined", "-I",
+                            os.path.join(root, "paper_2203_03341_amd", "csrc"), str(tmp_path / "sizes.cpp"), "-o", exe],
+                           capture_output=True, text=True)
+    assert built.returncode == 0, built.stderr
+    run = subprocess.run([exe], capture_output=True, text=True, timeout=60)
+    assert run.returncode == 0, run.stdout + run.stderr
+
+
+def test_tiles_of_groups_next_to_the_largest(tmp_path):
+    """What the kernels count from two 32-bit offsets: as many tiles as there are, up to the largest group there can be."""
+    _run_on_the_sizes(tmp_path, """
+      const int begins[] = {0, 1, 127, 128, 1 << 20};
+      for (int begin : begins)
+        for (long long columns : {0ll, 1ll, 127ll, 128ll, 129ll, 2147483519ll, 2147483520ll, 2147483521ll, 2147483646ll, 2147483647ll}) {
+          if (begin + columns > 2147483647ll) continue;
+          const int end = (int)(begin + columns);
+          const long long tiles = grouped_tiles(end - begin);
+          CHECK(tiles >= 0 && tiles * 128 >= columns && (tiles - 1) * 128 < columns);
+        }
+      CHECK(grouped_tiles(2147483521) == 16777216);
+    """)
+
+
+def test_kernels_count_tiles_nowhere_else():
+    """The tiles of a group are counted by the function tested above, on either side."""
+    import glob
+    import os
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    files = glob.glob(os.path.join(root, "paper_2203_03341_amd", "csrc", "grouped_*.hpp"))
+    text = {os.path.basename(f): open(f).read() for f in files}
+    assert "grouped_tiles(end - begin)" in text["grouped_kernel.hpp"]
+    assert [f for f, t in text.items() if "kGroupedTile - 1) / kGroupedTile" in t] == ["grouped_sizes.hpp"]
