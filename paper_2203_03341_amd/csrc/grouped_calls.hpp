@@ -85,7 +85,7 @@ ecgemm_status_t launch_grouped(ecgemm_handle_t h, ecgemm_mode_t mode, bool depth
 
 // The kernels for few columns to a group (narrow_kernel.hpp).
 constexpr int64_t kAdapterDownMeanColumns = 8, kNarrowProjectionColumns = 64;
-constexpr int64_t kNarrowTallBlocks = 256, kShallowMeanDepth = 16, kShallowMeanDepthSlim = 64;
+constexpr int64_t kShallowMeanDepth = 16, kShallowMeanDepthSlim = 64;
 constexpr int64_t kAdapterOneLaunchDepth = 6144, kAdapterOneLaunchChunks = 8, kAdapterOneLaunchTiles = 128;
 
 // Whether ecgemm_sgemm_grouped runs on narrow_kernel, by what either kernel is estimated to take (us), all groups taken as
@@ -122,15 +122,6 @@ bool narrow_projection_is_faster(bool depth_a, int64_t M, int64_t N, int64_t K, 
   const double pass_us = std::max(4.0 * M * K / 4.7e6, K / 1024.0 * (depth_a ? 2.9 : 9.3));
   return 4.0 + std::ceil((double)N / kNarrowColumns) * pass_us < other_us;
 }
-
-// Blocks of 16 rows the operand that is read once is taken in: four where its rows are contiguous, else two where that leaves
-// enough blocks and there are enough columns for it to matter (4096 deep times 32 columns, 8192 rows 49.6 us / 33.8 with 32 rows
-// a block, 4096 rows 25.5 / 33.5).
-int narrow_fr(bool depth, int64_t groups, int64_t rows, int64_t columns) {
-  return !depth ? 4 : columns > 16 && groups * ((rows + 31) / 32) >= kNarrowTallBlocks ? 2 : 1;
-}
-int64_t narrow_row_blocks(int fr, int64_t rows) { return (rows + 16 * fr - 1) / (16 * fr); }
-bool narrow_fits(int64_t groups, int64_t M) { return (groups + 1) * narrow_row_blocks(1, M) <= INT_MAX; }
 
 ecgemm_status_t launch_narrow(ecgemm_handle_t h, bool depth_a, bool depth_b, NarrowParams np) {
   const int64_t groups = np.offsets ? np.groups : 1;
@@ -197,7 +188,7 @@ ecgemm_status_t ecgemm_sgemm_grouped(ecgemm_handle_t handle, ecgemm_op_t transA,
   }
   const OnDeviceOf device(h);
   if (device.error != hipSuccess) return hip_fail(h, device.error, "hipSetDevice");
-  if (narrow_is_faster(transA == ECGEMM_OP_T, groups, M, N, K, mode) && narrow_fits(groups, M)) {
+  if (narrow_is_faster(transA == ECGEMM_OP_T, groups, M, N, K, mode) && narrow_fits(transA == ECGEMM_OP_T, groups, M, N / groups, 0)) {
     NarrowParams np{};
     np.A = A, np.lda = lda, np.stride_a = strideA;
     np.B = B, np.ldb = ldb;
@@ -253,13 +244,12 @@ ecgemm_status_t ecgemm_sgemm_grouped_depth(ecgemm_handle_t handle, ecgemm_op_t t
   }
   const OnDeviceOf device(h);
   if (device.error != hipSuccess) return hip_fail(h, device.error, "hipSetDevice");
-  const int64_t row_blocks = (M + 255) / 256, column_blocks = (N + kShallowColumns - 1) / kShallowColumns;
   // Shallow groups, by their mean depth.  Tiles / shallow, us, FP16, groups of M x N: 64 of 1024 x 768, of depth 1 66 / 58, 16 66 /
   // 55, 32 66 / 63 and 97 / 112 with beta; 51 of 1792 x 1216, 1 146 / 110, 16 146 / 119, 32 146 / 158; 4 of 4096 x 4096, 1 86 / 60, 32 87 /
   // 77, 48 87 / 99; 11 of 320 x 1664, 16 16 / 13.6, 32 with beta 20 / 28.  One side of 64 or less, which a tile only half fills: 8 of
   // 64 x 4096, 1 10.1 / 5.9, 64 9.6 / 7.8, 128 10.3 / 11.7; 4096 x 64 alike.
   const int64_t shallow = M <= 64 || N <= 64 ? kShallowMeanDepthSlim : kShallowMeanDepth;
-  if (K <= shallow * groups && row_blocks * column_blocks <= INT_MAX / groups) {
+  if (K <= shallow * groups && shallow_fits(groups, M, N)) {
     ShallowParams sp{};
     sp.A = A, sp.lda = lda;
     sp.B = B, sp.ldb = ldb;
@@ -267,12 +257,12 @@ ecgemm_status_t ecgemm_sgemm_grouped_depth(ecgemm_handle_t handle, ecgemm_op_t t
     sp.M = M, sp.N = N, sp.K = K;
     sp.offsets = offsets;
     sp.alpha = alpha, sp.beta = beta;
-    sp.row_blocks = (int)row_blocks, sp.column_blocks = (int)column_blocks;
+    sp.row_blocks = (int)shallow_row_blocks(M), sp.column_blocks = (int)shallow_column_blocks(N);
     static void (*const kernels[2][2])(ShallowParams) = {{shallow_kernel<false, false>, shallow_kernel<false, true>},
                                                          {shallow_kernel<true, false>, shallow_kernel<true, true>}};
     void* args[] = {&sp};
     ECGEMM_HIP(h, hipLaunchKernel(reinterpret_cast<const void*>(kernels[transA == ECGEMM_OP_T][transB == ECGEMM_OP_N]),
-                                  dim3((unsigned)(groups * row_blocks * column_blocks)), dim3(256), args, 0, h->stream));
+                                  dim3((unsigned)(groups * (shallow_row_blocks(M) * shallow_column_blocks(N)))), dim3(kShallowThreads), args, 0, h->stream));
     return ECGEMM_OK;
   }
   GroupedParams gp{};
@@ -359,7 +349,8 @@ ecgemm_status_t ecgemm_sgemm_adapters(ecgemm_handle_t handle, ecgemm_op_t transA
     if (M == 0) return ECGEMM_OK;
     return sgemm_common(h, transA, transB, M, N, K, alpha, A, lda, B, ldb, beta, C, ldc, mode, nullptr, nullptr, kWorkspaceOfHandle);
   }
-  const bool narrow = project && lda <= kGroupedLargestLd && narrow_projection_is_faster(transA == ECGEMM_OP_T, M, N, K, mode);
+  const bool narrow = project && lda <= kGroupedLargestLd && narrow_projection_is_faster(transA == ECGEMM_OP_T, M, N, K, mode) &&
+                      narrow_fits(transA == ECGEMM_OP_T, 1, M, N, 0);
   // Projection and adapters in one launch, where both matrices and H are laid out alike (see grouped_kernel), there are tiles
   // enough for half the chip, no more than a few adapters meet in a tile, and the projection is not so deep that splitting
   // first outweighs two passes over C.  Whole calls so / with C written first and the projection added, us, FP16, M x N x K,
@@ -371,8 +362,13 @@ ecgemm_status_t ecgemm_sgemm_adapters(ecgemm_handle_t handle, ecgemm_op_t transA
   const bool one_launch = project && !narrow && transA == transU && depth_b && groups <= kGroupsPerLaunch && lda <= kGroupedLargestLd &&
                           h->log2_scale_a == 0 && h->log2_scale_b == 0 && K <= kAdapterOneLaunchDepth && tiles >= kAdapterOneLaunchTiles && added_chunks <= kAdapterOneLaunchChunks &&
                           std::fabs(alpha) >= 0x1p-16f && std::fabs(alpha) <= 0x1p16f;  // (H is multiplied by scales / alpha)
-  const int64_t up_columns = N < 2 * kAdapterUpColumnsShort * groups ? kAdapterUpColumnsShort : kAdapterUpColumns;
-  ECGEMM_ARG(h, (M + 255) / 256 * ((N + up_columns - 1) / up_columns) > INT_MAX, 4, "ecgemm_sgemm_adapters: M x N too large");
+  // The launches for H and for C before the projection, refused before the first of them where they cannot hold the call
+  const bool narrow_down = N < kAdapterDownMeanColumns * groups && narrow_fits(transD == ECGEMM_OP_T, groups, rank, N / groups, 1);
+  const int down_fr = narrow_fr(depth_b, 1, N, rank);
+  ECGEMM_ARG(h, !narrow_down && !launchable(narrow_row_blocks(down_fr, N), kNarrowThreads), 5, "ecgemm_sgemm_adapters: N too large");
+  const bool few = N < 2 * kAdapterUpColumnsShort * groups && launchable(adapter_up_blocks(M, N, kAdapterUpColumnsShort), kAdapterUpThreads);
+  const int64_t up_blocks = adapter_up_blocks(M, N, few ? kAdapterUpColumnsShort : kAdapterUpColumns);
+  ECGEMM_ARG(h, M > 0 && !narrow && !one_launch && !launchable(up_blocks, kAdapterUpThreads), 4, "ecgemm_sgemm_adapters: M x N too large");
   if (project && !narrow && !one_launch) {  // what the projection would refuse is refused before anything is enqueued
     st = check_sizes(h, M, N, K, mode, 4);
     if (st != ECGEMM_OK) return st;
@@ -383,7 +379,7 @@ ecgemm_status_t ecgemm_sgemm_adapters(ecgemm_handle_t handle, ecgemm_op_t transA
     if (st != ECGEMM_OK) return st;
   }
   // H = op(D) op(B), zero in every column without an adapter: few columns to a group, the adapters are read once, else B is
-  if (N < kAdapterDownMeanColumns * groups && narrow_fits(groups, rank)) {
+  if (narrow_down) {
     NarrowParams down{};
     down.A = D, down.lda = ldd, down.stride_a = strideD;
     down.B = B, down.ldb = ldb;
@@ -403,13 +399,13 @@ ecgemm_status_t ecgemm_sgemm_adapters(ecgemm_handle_t handle, ecgemm_op_t transA
     down.offsets = offsets, down.groups = groups;
     down.index = index, down.matrices = (int)adapters;
     down.H = H, down.ldh = ldh;
-    const int fr = narrow_fr(depth_b, 1, N, rank);
     const bool depth_d = transD == ECGEMM_OP_T;
-    void (*const kernel)(AdapterDownParams) = fr == 4   ? (depth_d ? adapter_down_kernel<false, true, 4> : adapter_down_kernel<false, false, 4>)
-                                              : fr == 2 ? (depth_d ? adapter_down_kernel<true, true, 2> : adapter_down_kernel<true, false, 2>)
-                                                        : (depth_d ? adapter_down_kernel<true, true, 1> : adapter_down_kernel<true, false, 1>);
+    void (*const kernel)(AdapterDownParams) = down_fr == 4 ? (depth_d ? adapter_down_kernel<false, true, 4> : adapter_down_kernel<false, false, 4>)
+                                              : down_fr == 2
+                                                  ? (depth_d ? adapter_down_kernel<true, true, 2> : adapter_down_kernel<true, false, 2>)
+                                                  : (depth_d ? adapter_down_kernel<true, true, 1> : adapter_down_kernel<true, false, 1>);
     void* args[] = {&down};
-    ECGEMM_HIP(h, hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)narrow_row_blocks(fr, N), groups > 1 ? 2 : 1),
+    ECGEMM_HIP(h, hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)narrow_row_blocks(down_fr, N), groups > 1 ? 2 : 1),
                                   dim3(kNarrowThreads), args, 0, h->stream));
   }
   if (M == 0) return ECGEMM_OK;
@@ -458,15 +454,14 @@ ecgemm_status_t ecgemm_sgemm_adapters(ecgemm_handle_t handle, ecgemm_op_t transA
   up.offsets = offsets, up.groups = groups;
   up.index = index, up.matrices = (int)adapters;
   up.scales = scales, up.beta = beta;
-  up.row_blocks = (int)((M + 255) / 256);
+  up.row_blocks = (int)adapter_up_row_blocks(M);
   // Few columns to a request: a block's runs follow each other at 2 us each.  Calls with 64 / 8 columns a block, 128 requests of
   // a column, rank 16: 4096 x 4096 170 us / 53, 1024 x 2048 150 / 30; 512 of a column, 8192 x 2048, 198 / 108.
-  const bool few = up_columns == kAdapterUpColumnsShort;
   void (*const up_kernel)(AdapterUpParams) =
       transU == ECGEMM_OP_T ? (few ? adapter_up_kernel<true, kAdapterUpColumnsShort> : adapter_up_kernel<true, kAdapterUpColumns>)
                             : (few ? adapter_up_kernel<false, kAdapterUpColumnsShort> : adapter_up_kernel<false, kAdapterUpColumns>);
   void* up_args[] = {&up};
-  ECGEMM_HIP(h, hipLaunchKernel(reinterpret_cast<const void*>(up_kernel), dim3((unsigned)(up.row_blocks * ((N + up_columns - 1) / up_columns))), dim3(256), up_args,
+  ECGEMM_HIP(h, hipLaunchKernel(reinterpret_cast<const void*>(up_kernel), dim3((unsigned)up_blocks), dim3(kAdapterUpThreads), up_args,
                                 0, h->stream));
   if (!project) return ECGEMM_OK;
   return sgemm_common(h, transA, transB, M, N, K, alpha, A, lda, B, ldb, 1.0f, C, ldc, mode, nullptr, nullptr, kWorkspaceOfHandle);

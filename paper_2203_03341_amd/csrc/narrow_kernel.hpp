@@ -211,7 +211,6 @@ struct WaveProduct {
 };
 
 // The block's sums over the whole depth, in `sums`[column][row] (ROWS + 1 apart): all waves' partial sums in order.
-constexpr int kNarrowWaves = 8, kNarrowThreads = 64 * kNarrowWaves;
 template <bool S_DEPTH, bool T_DEPTH, int FR, bool WIDE>
 union NarrowSums {
   float space[kNarrowWaves][WaveProduct<S_DEPTH, T_DEPTH, FR, WIDE ? 4 : 2>::SPACE + 4];  // while the waves multiply
@@ -420,7 +419,6 @@ __global__ void __launch_bounds__(kNarrowThreads, 2) adapter_down_kernel(const A
   }
 }
 
-constexpr int kAdapterUpColumns = 64, kAdapterUpColumnsShort = 8;
 // The second half: C = scales[a] op(U_a) H + beta C in every column, before the projection is added.  A block takes 256 rows
 // of C and 64 columns (8 where there are few to a request), a wave 64 rows, run by run of columns with the same adapter; the
 // depth is the rank.  Bound by writing C (and by reading it, unless beta is zero).
@@ -438,14 +436,14 @@ struct AdapterUpParams {
   int row_blocks;
 };
 template <bool DEPTH_U, int COLUMNS>
-__global__ void __launch_bounds__(256) adapter_up_kernel(const AdapterUpParams p) {
+__global__ void __launch_bounds__(kAdapterUpThreads) adapter_up_kernel(const AdapterUpParams p) {
   __shared__ int adapter[(COLUMNS + kNarrowColumns - 1) / kNarrowColumns][kNarrowColumns];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t n0 = (int64_t)(blockIdx.x / (unsigned)p.row_blocks) * COLUMNS;
-  const int64_t m0 = (int64_t)(blockIdx.x % (unsigned)p.row_blocks) * 256 + 64 * wave;
+  const int64_t m0 = (int64_t)(blockIdx.x % (unsigned)p.row_blocks) * kAdapterUpRows + 64 * wave;
   const int cols = (int)(p.N - n0 < COLUMNS ? p.N - n0 : COLUMNS);
   for (int i = 0; i * kNarrowColumns < cols; ++i)
-    find_adapters(p.offsets, p.groups, p.index, p.matrices, p.N, n0 + i * kNarrowColumns, kNarrowColumns, adapter[i], 256);
+    find_adapters(p.offsets, p.groups, p.index, p.matrices, p.N, n0 + i * kNarrowColumns, kNarrowColumns, adapter[i], kAdapterUpThreads);
   if (m0 >= p.M) return;
   const int rows = (int)(p.M - m0 < 64 ? p.M - m0 : 64);
   auto adapter_of = [&](int c) { return uniform(adapter[c / kNarrowColumns][c % kNarrowColumns]); };
@@ -511,9 +509,8 @@ struct ShallowParams {
   float* C;
   int row_blocks, column_blocks;
 };
-constexpr int kShallowColumns = 64;
 template <bool DEPTH_A, bool DEPTH_B>
-__global__ void __launch_bounds__(256) shallow_kernel(const ShallowParams p) {
+__global__ void __launch_bounds__(kShallowThreads) shallow_kernel(const ShallowParams p) {
   constexpr int NF = kShallowColumns / 16;
   typedef WaveProduct<DEPTH_A, DEPTH_B, 4, NF, true> Product;
   __shared__ __attribute__((aligned(16))) float space[4][Product::SPACE + 4];
@@ -528,7 +525,7 @@ __global__ void __launch_bounds__(256) shallow_kernel(const ShallowParams p) {
   }
   __syncthreads();
   const int64_t begin = uniform(range[0]), depth = uniform(range[1]) - begin;
-  const int64_t m0 = (int64_t)(block % (unsigned)p.row_blocks) * 256 + 64 * wave, n0 = (int64_t)(block / (unsigned)p.row_blocks) * kShallowColumns;
+  const int64_t m0 = (int64_t)(block % (unsigned)p.row_blocks) * kShallowRows + 64 * wave, n0 = (int64_t)(block / (unsigned)p.row_blocks) * kShallowColumns;
   if (m0 >= p.M) return;
   const int rows = (int)(p.M - m0 < 64 ? p.M - m0 : 64), cols = (int)(p.N - n0 < kShallowColumns ? p.N - n0 : kShallowColumns);
   narrow_acc_t acc[4][NF];

@@ -860,3 +860,71 @@ def test_one_group_of_the_most_columns_there_can_be(handle):
     assert bool((C[:guard] == 7.0).all()) and bool((C[guard + N:] == 7.0).all())
     step = 1 << 28
     assert all(bool((C[guard + at:min(guard + at + step, guard + N)] == 3.0).all()) for at in range(0, N, step))
+
+
+def test_calls_that_no_single_launch_holds(handle):
+    """More groups than one launch of the kernel that suits their size: another one makes them."""
+    import torch
+    ec, gen = _ec(), _gen(41)
+    # 131072 groups of a column each, one matrix for all
+    G, M, K = 131072, 1024, 16
+    A, x = torch.randn((M, K), generator=gen, device="cuda"), torch.randn((G, K), generator=gen, device="cuda")
+    y = torch.full((G, M), 7.0, device="cuda")
+    offs = torch.arange(G + 1, device="cuda")
+    handle.sgemm_grouped(ec.OP_T, ec.OP_N, G, M, G, K, 1.0, A, K, 0, x, K, offs, 0.0, y, M, ec.MODE_FP16_SPLIT)
+    torch.cuda.synchronize()
+    for at in range(0, G, 16384):
+        rows = slice(at, at + 16384)
+        allowed = _allowed(x[rows].double(), A.double().t().contiguous(), "fp16", 1.0, 0.0, None)
+        assert bool(((y[rows].double() - x[rows].double() @ A.double().t().contiguous()).abs() <= allowed).all())
+    # 2^24 gradients of one value
+    G = 1 << 24
+    x, g, c = torch.randn(G, generator=gen, device="cuda"), torch.randn(G, generator=gen, device="cuda"), torch.full((G,), 7.0, device="cuda")
+    handle.sgemm_grouped_depth(ec.OP_N, ec.OP_T, G, 1, 1, G, 1.0, x, 1, g, 1, torch.arange(G + 1, device="cuda"), 0.0, c, 1, 1, ec.MODE_BF16_FULL)
+    torch.cuda.synchronize()
+    exact = x.double() * g.double()     # one product: what _allowed gives for a depth of 1
+    assert bool(((c.double() - exact).abs() <= (2.0 ** -21 + 2 * (16 * 2.0 ** -25 + 2.0 ** -24) + 4 * 2.0 ** -24) * exact.abs() + 1e-37).all())
+
+
+def test_adapters_of_more_requests_than_a_launch_holds(handle):
+    import torch
+    ec, gen = _ec(), _gen(42)
+    G, M, K, R = 131072, 8, 16, 1024
+    x, W = torch.randn((G, K), generator=gen, device="cuda"), torch.randn((M, K), generator=gen, device="cuda")
+    D, U = torch.randn((2, R, K), generator=gen, device="cuda"), torch.randn((2, M, R), generator=gen, device="cuda") / 32
+    index = torch.randint(-1, 2, (G,), generator=gen, device="cuda", dtype=torch.int32)
+    y, H = torch.full((G, M), 7.0, device="cuda"), torch.full((G, R), 7.0, device="cuda")
+    handle.sgemm_adapters(ec.OP_T, ec.OP_N, M, G, K, 1.0, W, K, x, K, G, torch.arange(G + 1, device="cuda"), index, 2, R, ec.OP_T, D, K, R * K,
+                          ec.OP_T, U, R, M * R, None, H, R, 0.0, y, M, ec.MODE_FP16_SPLIT)
+    torch.cuda.synchronize()
+    for a in (-1, 0, 1):
+        rows = (index == a).nonzero()[:, 0]
+        b, h = x[rows].double(), H[rows]
+        exact, allowed = b @ W.double().t().contiguous(), _allowed(b, W.double().t().contiguous(), "fp16", 1.0, 0.0, None)
+        if a < 0:
+            assert bool((h == 0).all())
+        else:
+            d, u = D[a].double().t().contiguous(), U[a].double().t().contiguous()
+            want, h_allowed = b @ d, _allowed(b, d, "fp16", 1.0, 0.0, None)
+            assert bool(((h.double() - want).abs() <= h_allowed).all())
+            exact = exact + want @ u
+            allowed = allowed + h_allowed @ u.abs() + _allowed(want, u, "fp16", 1.0, 0.0, None) + 2.0 ** -23 * exact.abs()
+        assert bool(((y[rows].double() - exact).abs() <= allowed).all())
+
+
+def test_adapters_that_no_launch_holds_are_refused_before_anything_is_written(handle):
+    import torch
+    ec = _ec()
+    t = torch.zeros(4096, device="cuda")
+    offs, index = torch.zeros(4, dtype=torch.int64, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+
+    def call(M, N, alpha):
+        handle.sgemm_adapters(ec.OP_T, ec.OP_N, M, N, 8, alpha, t, 8, t, 8, 3, offs, index, 2, 4, ec.OP_T, t, 8, 32, ec.OP_T, t, 4, 32, None,
+                              t[2048:], 4, 0.0, t[3000:], M, ec.MODE_FP16_SPLIT)
+
+    for position, sizes in ((5, (8, 1 << 30, 1.0)), (4, ((1 << 31) - 1, 1024, 0.0))):
+        with pytest.raises(ec.EcgemmError) as err:
+            call(*sizes)
+        assert err.value.status == ec.ERR_INVALID_ARG and err.value.argument == position
+    torch.cuda.synchronize()
+    assert bool((t == 0).all())

@@ -79,3 +79,27 @@ def test_kernels_count_tiles_nowhere_else():
     text = {os.path.basename(f): open(f).read() for f in files}
     assert "grouped_tiles(end - begin)" in text["grouped_kernel.hpp"]
     assert [f for f, t in text.items() if "kGroupedTile - 1) / kGroupedTile" in t] == ["grouped_sizes.hpp"]
+
+
+def test_calls_go_only_to_launches_that_hold_them(tmp_path):
+    """A launch has fewer than 2^32 threads along x.  The kernels of few columns and shallow groups, from both sides of that."""
+    _run_on_the_sizes(tmp_path, """
+      CHECK(launchable(8388607, 512) && !launchable(8388608, 512) && launchable(16777215, 256) && !launchable(16777216, 256));
+      CHECK(!launchable((long long)1 << 62, 1));
+      // 131072 groups of 1024 rows, depth contiguous: 64 blocks of 16 rows each; rows contiguous: 16 of 64
+      CHECK(!narrow_fits(true, 131072, 1024, 1, 0) && narrow_fits(true, 131071, 1024, 1, 0) && !narrow_fits(true, 131071, 1024, 1, 1));
+      CHECK(narrow_fits(false, 131072, 1024, 1, 1) && !narrow_fits(false, 524288, 1024, 1, 0));
+      CHECK(!narrow_fits(true, 131072, 1024, 1, 1) && narrow_fits(true, 131072, 512, 1, 1));
+      CHECK(narrow_fits(true, 1, 134217712, 1, 0) && !narrow_fits(true, 1, 134217713, 1, 0) && narrow_fits(true, 1, 134217713, 17, 0));
+      CHECK(!narrow_fits(true, 2147483647, 2147483647, 1, 1));
+      // groups of one value, of 256 x 64, of 257 x 64
+      CHECK(!shallow_fits(16777216, 1, 1) && shallow_fits(16777215, 1, 1) && shallow_fits(16777215, 256, 64));
+      CHECK(!shallow_fits(16777215, 257, 64) && shallow_fits(8388607, 257, 64) && !shallow_fits(2147483647, 1 << 22, 1 << 22));
+      CHECK(adapter_up_blocks(257, 65, 64) == 4 && adapter_up_blocks(256, 64, 8) == 8);
+      CHECK(launchable(adapter_up_blocks(1 << 20, 262080, 64), 256) && !launchable(adapter_up_blocks(1 << 20, 262144, 64), 256));
+      CHECK(adapter_up_blocks(0, 5, 64) == 0);
+      // as many rows as the columns of adapters that a call of one launch can have
+      CHECK(launchable(narrow_row_blocks(narrow_fr(true, 1, 134217712, 16), 134217712), kNarrowThreads));
+      CHECK(!launchable(narrow_row_blocks(narrow_fr(true, 1, 134217713, 16), 134217713), kNarrowThreads));
+      CHECK(launchable(narrow_row_blocks(narrow_fr(false, 1, 536870848, 16), 536870848), kNarrowThreads));
+    """)
