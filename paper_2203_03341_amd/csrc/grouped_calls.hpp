@@ -55,22 +55,27 @@ ecgemm_status_t launch_grouped(ecgemm_handle_t h, ecgemm_mode_t mode, bool depth
                                   ? (scaled ? grouped_kernel_of<kMethodFp16Split, true>(depth_a, depth_b) : grouped_kernel_of<kMethodFp16Split, false>(depth_a, depth_b))
                                   : (scaled ? grouped_kernel_of<kMethodBf16Full, true>(depth_a, depth_b) : grouped_kernel_of<kMethodBf16Full, false>(depth_a, depth_b));
   const GroupedParams whole = gp;
+  // The workspace for whichever launch needs most (all but the last one have as many groups as a launch takes), before the
+  // first of them: a call that is refused leaves C as it was.
+  const int64_t depth = gp.along_depth ? gp.K / groups : gp.K;  // of a group, all taken as equal
+  size_t partial_bytes = 0;
+  for (const int64_t n : {std::min<int64_t>(groups, kGroupsPerLaunch), (groups - 1) % kGroupsPerLaunch + 1}) {
+    const int64_t tiles = most_grouped_tiles(gp.along_depth, n, gp.M, gp.N), slices = grouped_slices(tiles, depth);
+    if (slices > 1) partial_bytes = std::max(partial_bytes, (size_t)(slices * tiles) * kGroupedTile * kGroupedTile * sizeof(float));
+  }
+  char* ws = nullptr;
+  const ecgemm_status_t st = acquire_workspace(h, partial_bytes, &ws);
+  if (st != ECGEMM_OK) return st;
+  if (partial_bytes > 0) h->auto_choice = nullptr;  // (the workspace held it)
   for (int64_t first = 0; first < groups; first += kGroupsPerLaunch) {
     gp.groups = (int)std::min<int64_t>(groups - first, kGroupsPerLaunch);
     gp.offsets = whole.offsets + first;
     gp.A = whole.A + first * whole.stride_a;
     gp.C = whole.C + first * whole.stride_c;
     const int64_t tiles = most_grouped_tiles(gp.along_depth, gp.groups, gp.M, gp.N);
-    gp.slices = grouped_slices(tiles, gp.along_depth ? gp.K / gp.groups : gp.K);
+    gp.slices = grouped_slices(tiles, depth);
     gp.partial_tiles = tiles;
-    gp.partials = nullptr;
-    if (gp.slices > 1) {
-      char* ws = nullptr;
-      const ecgemm_status_t st = acquire_workspace(h, (size_t)gp.slices * tiles * kGroupedTile * kGroupedTile * sizeof(float), &ws);
-      if (st != ECGEMM_OK) return st;
-      h->auto_choice = nullptr;  // (the workspace held it)
-      gp.partials = reinterpret_cast<float*>(ws);
-    }
+    gp.partials = gp.slices > 1 ? reinterpret_cast<float*>(ws) : nullptr;
     const int64_t items = tiles * gp.slices;
     const int64_t grid = std::max(std::min<int64_t>(items, h->compute_units), (items + kGroupedTilesPerBlock - 1) / kGroupedTilesPerBlock);
     void* args[] = {&gp};

@@ -928,3 +928,30 @@ def test_adapters_that_no_launch_holds_are_refused_before_anything_is_written(ha
         assert err.value.status == ec.ERR_INVALID_ARG and err.value.argument == position
     torch.cuda.synchronize()
     assert bool((t == 0).all())
+
+
+@pytest.mark.parametrize("mode", MODES)
+def test_the_last_of_several_launches_takes_its_groups_for_as_deep_as_they_are(handle, mode):
+    """1025 groups are two launches, the second one of a single group.  A hundred deep each, they are cut into no slices, so that a
+    caller's workspace of any size does; two thousand deep, the last one is, and a workspace too small for it is refused before
+    anything is written."""
+    import torch
+    ec, G = _ec(), 1025
+    own = ec.Handle()
+    own.set_stream(torch.cuda.current_stream().cuda_stream)
+    small = torch.empty(256, dtype=torch.uint8, device="cuda")
+    own.set_workspace(small, 256)
+    _run_depth(own, "NT", mode, 65, 66, [100] * G)
+    M, N, K = 65, 66, 2048 * G
+    A, B, C = torch.ones((K, M), device="cuda"), torch.ones((K, N), device="cuda"), torch.full((G, N, M), 7.0, device="cuda")
+    args = (ec.OP_N, ec.OP_T, G, M, N, K, 1.0, A, M, B, N, torch.arange(G + 1, device="cuda") * 2048, 1.0, C, M, M * N, _mode(mode))
+    with pytest.raises(ec.EcgemmError) as err:
+        own.sgemm_grouped_depth(*args)
+    assert err.value.status == ec.ERR_ALLOC
+    torch.cuda.synchronize()
+    assert bool((C == 7.0).all())
+    own.set_workspace(None, 0)
+    own.sgemm_grouped_depth(*args)
+    torch.cuda.synchronize()
+    assert bool((C == 2055.0).all())        # (sums of ones: exact)
+    own.destroy()
