@@ -2,7 +2,8 @@
 
 The functions mirror include/ecgemm.h one to one.  Matrices are torch CUDA tensors used purely as
 device memory: a column-major (ld, cols) matrix is any float32 tensor whose storage holds it, and
-the binding passes `data_ptr()` straight through.  There is no CPU fallback: if the shared library
+the binding passes `data_ptr()` straight through (the grouped products, whose tables are easily had in another type,
+look at the operands' types first).  There is no CPU fallback: if the shared library
 is missing or fails to load, importing this module raises.
 """
 from __future__ import annotations
@@ -121,6 +122,29 @@ def _ptr(t) -> int:
     return t.data_ptr()
 
 
+def _typed(t, name: str, position: int, dtype, count=None) -> int:
+    """_ptr of an operand of the grouped products.  Kernels take the bytes for what they expect: a tensor of another type or on
+    another kind of device is refused, and so is a table (`count` entries) that is too short or has gaps.  An address is taken
+    as it is.  `position` is the argument's in the C function, the handle being the first."""
+    if t is None or isinstance(t, int):
+        return t or 0
+    if t.dtype is not dtype:
+        raise EcgemmError(ERR_INVALID_ARG, f"{name}: {dtype} expected, got {t.dtype}", position)
+    # (a count beyond 32 bits is the library's to refuse)
+    if count is not None and count < 1 << 31 and (t.numel() < count or not t.is_contiguous()):
+        raise EcgemmError(ERR_INVALID_ARG, f"{name}: {count} contiguous entries expected, got {tuple(t.shape)} with strides {t.stride()}", position)
+    if not t.is_cuda:
+        raise EcgemmError(ERR_INVALID_ARG, f"{name}: on {t.device}, not in GPU memory", position)
+    return t.data_ptr()
+
+
+try:
+    import torch
+    _FLOAT, _INT64, _INT32 = torch.float32, torch.int64, torch.int32
+except ImportError:     # operands are addresses, then
+    _FLOAT = _INT64 = _INT32 = None
+
+
 class Handle:
     """Owns one ecgemm_handle_t.  Methods have the names and argument order of the C functions."""
 
@@ -197,23 +221,28 @@ class Handle:
     def sgemm_grouped(self, transA: int, transB: int, groups: int, M: int, N: int, K: int, alpha: float, A, lda: int, strideA: int,
                       B, ldb: int, offsets, beta: float, C, ldc: int, mode: int):
         """offsets: int64 tensor of groups + 1 entries on the device."""
-        self._check(_lib.ecgemm_sgemm_grouped(self._h, transA, transB, groups, M, N, K, alpha, _ptr(A), lda, strideA, _ptr(B), ldb,
-                                              _ptr(offsets), beta, _ptr(C), ldc, mode))
+        self._check(_lib.ecgemm_sgemm_grouped(self._h, transA, transB, groups, M, N, K, alpha, _typed(A, "A", 9, _FLOAT), lda, strideA,
+                                              _typed(B, "B", 12, _FLOAT), ldb, _typed(offsets, "offsets", 14, _INT64, groups + 1), beta,
+                                              _typed(C, "C", 16, _FLOAT), ldc, mode))
 
     def sgemm_grouped_depth(self, transA: int, transB: int, groups: int, M: int, N: int, K: int, alpha: float, A, lda: int, B, ldb: int,
                             offsets, beta: float, C, ldc: int, strideC: int, mode: int):
         """offsets: int64 tensor of groups + 1 entries on the device."""
-        self._check(_lib.ecgemm_sgemm_grouped_depth(self._h, transA, transB, groups, M, N, K, alpha, _ptr(A), lda, _ptr(B), ldb,
-                                                    _ptr(offsets), beta, _ptr(C), ldc, strideC, mode))
+        self._check(_lib.ecgemm_sgemm_grouped_depth(self._h, transA, transB, groups, M, N, K, alpha, _typed(A, "A", 9, _FLOAT), lda,
+                                                    _typed(B, "B", 11, _FLOAT), ldb, _typed(offsets, "offsets", 13, _INT64, groups + 1), beta,
+                                                    _typed(C, "C", 15, _FLOAT), ldc, strideC, mode))
 
     def sgemm_adapters(self, transA: int, transB: int, M: int, N: int, K: int, alpha: float, A, lda: int, B, ldb: int, groups: int,
                        offsets, index, adapters: int, rank: int, transD: int, D, ldd: int, strideD: int, transU: int, U, ldu: int,
                        strideU: int, scales, H, ldh: int, beta: float, C, ldc: int, mode: int):
         """offsets: int64 tensor of groups + 1 entries, index: int32 tensor of groups entries, scales: float32 tensor of
         adapters entries or None, all on the device."""
-        self._check(_lib.ecgemm_sgemm_adapters(self._h, transA, transB, M, N, K, alpha, _ptr(A), lda, _ptr(B), ldb, groups,
-                                               _ptr(offsets), _ptr(index), adapters, rank, transD, _ptr(D), ldd, strideD, transU,
-                                               _ptr(U), ldu, strideU, _ptr(scales), _ptr(H), ldh, beta, _ptr(C), ldc, mode))
+        self._check(_lib.ecgemm_sgemm_adapters(self._h, transA, transB, M, N, K, alpha, _typed(A, "A", 8, _FLOAT), lda,
+                                               _typed(B, "B", 10, _FLOAT), ldb, groups, _typed(offsets, "offsets", 13, _INT64, groups + 1),
+                                               _typed(index, "index", 14, _INT32, groups), adapters, rank, transD,
+                                               _typed(D, "D", 18, _FLOAT), ldd, strideD, transU, _typed(U, "U", 22, _FLOAT), ldu, strideU,
+                                               _typed(scales, "scales", 25, _FLOAT, adapters), _typed(H, "H", 26, _FLOAT), ldh, beta,
+                                               _typed(C, "C", 29, _FLOAT), ldc, mode))
 
     def row_scales(self, op: int, rows: int, depth: int, src, ld: int, target_exponent: int, log2_scale):
         self._check(_lib.ecgemm_row_scales(self._h, op, rows, depth, _ptr(src), ld, target_exponent, _ptr(log2_scale)))

@@ -103,3 +103,60 @@ def test_calls_go_only_to_launches_that_hold_them(tmp_path):
       CHECK(!launchable(narrow_row_blocks(narrow_fr(true, 1, 134217713, 16), 134217713), kNarrowThreads));
       CHECK(launchable(narrow_row_blocks(narrow_fr(false, 1, 536870848, 16), 536870848), kNarrowThreads));
     """)
+
+
+def _calls():
+    """Of each method: its arguments by name, sound but for the null handle and operands that are not on a GPU"""
+    import torch
+    f, offs, index = torch.zeros(4096), torch.zeros(4, dtype=torch.int64), torch.zeros(3, dtype=torch.int32)
+    values = dict(transA=1, transB=0, groups=3, M=8, N=8, K=8, alpha=1.0, A=f, lda=8, strideA=64, B=f, ldb=8, offsets=offs, beta=0.0, C=f, ldc=8,
+                  strideC=64, mode=0, index=index, adapters=2, rank=4, transD=1, D=f, ldd=8, strideD=32, transU=1, U=f, ldu=4, strideU=32,
+                  scales=torch.ones(2), H=f, ldh=4)
+    import paper_2203_03341_amd as ec
+    for name in ("sgemm_grouped", "sgemm_grouped_depth", "sgemm_adapters"):
+        order = list(inspect.signature(getattr(ec.Handle, name)).parameters)[1:]
+        yield name, {k: values[k] for k in order}
+
+
+def test_operands_of_the_wrong_type_length_or_device_are_refused():
+    """Before the library sees an address: index in torch's default type, offsets in 32 bits, tables that end too early or have
+    gaps, weights in another type, what lies in host memory."""
+    import pytest
+    import torch
+    import paper_2203_03341_amd as ec
+    handle = ec.Handle.__new__(ec.Handle)
+    handle._h = None
+    wrong = {"offsets": [torch.zeros(4, dtype=torch.int32), torch.zeros(4), torch.zeros(3, dtype=torch.int64), torch.zeros(8, dtype=torch.int64)[::2]],
+             "index": [torch.zeros(3, dtype=torch.int64), torch.zeros(2, dtype=torch.int32), torch.zeros(6, dtype=torch.int32)[::2]],
+             "scales": [torch.ones(2, dtype=torch.float64), torch.ones(1), torch.ones(4)[::2]]}
+    for operand in "ABCDUH":
+        wrong[operand] = [torch.zeros(4096, dtype=t) for t in (torch.float64, torch.float16, torch.bfloat16, torch.int32)]
+    for name, sound in _calls():
+        order = list(sound)
+        on_gpu = {k: 4096 if isinstance(v, torch.Tensor) else v for k, v in sound.items()}      # (addresses are taken as they are)
+        with pytest.raises(ec.EcgemmError) as err:
+            getattr(handle, name)(*on_gpu.values())
+        assert "null handle" in str(err.value)      # got as far as the library
+        for operand, values in wrong.items():
+            if operand not in sound:
+                continue
+            for value in [*values, sound[operand]]:     # (the last: of the right type, in host memory)
+                with pytest.raises(ec.EcgemmError) as err:
+                    getattr(handle, name)(*{**on_gpu, operand: value}.values())
+                assert err.value.status == ec.ERR_INVALID_ARG and err.value.argument == order.index(operand) + 2, (name, operand, err.value)
+                assert operand + ":" in str(err.value)
+
+
+def test_counts_that_the_library_refuses_are_left_to_it():
+    """A negative or far too large number of groups or adapters is that argument's fault, not its table's."""
+    import pytest
+    import torch
+    from paper_2203_03341_amd import binding
+    table = torch.zeros(4, dtype=torch.int64)
+    for count in (-(1 << 62), -1, 0, 1 << 31, (1 << 31) + 1, 1 << 62):
+        with pytest.raises(binding.EcgemmError) as err:
+            binding._typed(table, "offsets", 14, torch.int64, count)
+        assert "not in GPU memory" in str(err.value)     # (its length was not what is wrong)
+    with pytest.raises(binding.EcgemmError) as err:
+        binding._typed(table, "offsets", 14, torch.int64, (1 << 31) - 1)
+    assert "contiguous entries" in str(err.value)
