@@ -376,9 +376,13 @@ ecgemm_status_t ecgemm_sgemm_grouped_depth(ecgemm_handle_t handle, ecgemm_op_t t
  *   U_a = U + a strideU: op(U_a) is M x rank, ldu >= (transU == N ? M : rank)
  *   scales: device, one factor per adapter; NULL: 1.
  *   H: device, FP32, rank x N column-major, ldh >= rank; written for all N columns.  It is an output because the backward
- *      pass needs it: with G the gradient of C, the gradient of op(B) is this same call on G with op(A)^T in A's place, U^T in
- *      D's and D^T in U's, which leaves U^T G in its H; the gradients of U and D are ecgemm_sgemm_grouped_depth of G with H,
- *      and of that call's H with B.
+ *      pass needs it.  With G the gradient of C:
+ *        op(B)   this same call on G with op(A)^T in A's place, U^T in D's and D^T in U's, which leaves G' = op(U_a)^T G in its H
+ *        op(U_a) scales[a] times the sum, over the groups g with index[g] = a, of G(:, j's of g) H(:, j's of g)^T
+ *        op(D_a) scales[a] times the sum, over the same groups, of G'(:, j's of g) op(B)(:, j's of g)^T
+ *      ecgemm_sgemm_grouped_depth with these groups gives the product of each group, without scales[a] (its alpha is one factor
+ *      for all of them): the caller multiplies by it, adds up the groups that share an adapter, and drops those that have none.
+ *      Where columns lie in the order of their adapters, one group for each adapter gives the sums themselves.
  * H times scales[a] / alpha is an operand like B: in FP16 mode it should lie in the window of the FP16 pair as well.  An adapter
  * that holds infinite or NaN values reaches its own columns only.
  * rank at most 1024; adapters below 2^31.  The projection uses the handle's workspace as ecgemm_sgemm does

@@ -955,3 +955,64 @@ def test_the_last_of_several_launches_takes_its_groups_for_as_deep_as_they_are(h
     torch.cuda.synchronize()
     assert bool((C == 2055.0).all())        # (sums of ones: exact)
     own.destroy()
+
+
+@pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("sizes,index", [([50, 0, 60, 33, 1, 27, 40], [2, 1, 0, -1, 2, 0, 5]), ([5, 70, 3], [0, 0, 0]), ([40, 50], [-1, 3])])
+def test_gradients_of_adapters_that_requests_share(handle, mode, sizes, index):
+    """Every adapter with a scale of its own, adapters that several requests share, that one has and that none has, requests without
+    one, rows of no request: the gradients of the input, of D and of U as the interface says they are made, against autograd in 64
+    bits and against differences."""
+    import torch
+    ec, gen, A, E = _ec(), _gen(51), 4, len(sizes)
+    K, M, R, start = 120, 88, 8, 2
+    T = start + sum(sizes) + 3
+    offs, ids = _offsets(sizes, start), torch.tensor(index, dtype=torch.int32, device="cuda")
+    x, gy = torch.randn((T, K), generator=gen, device="cuda"), torch.randn((T, M), generator=gen, device="cuda")
+    W = torch.randn((M, K), generator=gen, device="cuda") / K ** 0.5
+    D, U = torch.randn((A, R, K), generator=gen, device="cuda") / K ** 0.5, torch.randn((A, M, R), generator=gen, device="cuda") / R ** 0.5
+    scales = torch.tensor([0.5, -1.25, 2.0, 3.0], device="cuda")
+    y, H = torch.empty((T, M), device="cuda"), torch.empty((T, R), device="cuda")
+    gx, gH = torch.empty((T, K), device="cuda"), torch.empty((T, R), device="cuda")
+    handle.sgemm_adapters(ec.OP_T, ec.OP_N, M, T, K, 1.0, W, K, x, K, E, offs, ids, A, R, ec.OP_T, D, K, R * K, ec.OP_T, U, R, M * R, scales,
+                          H, R, 0.0, y, M, _mode(mode))
+    handle.sgemm_adapters(ec.OP_N, ec.OP_N, K, T, M, 1.0, W, K, gy, M, E, offs, ids, A, R, ec.OP_N, U, R, M * R, ec.OP_N, D, K, R * K, scales,
+                          gH, R, 0.0, gx, K, _mode(mode))
+    of_group_d, of_group_u = torch.empty((E, R, K), device="cuda"), torch.empty((E, M, R), device="cuda")
+    handle.sgemm_grouped_depth(ec.OP_N, ec.OP_T, E, K, R, T, 1.0, x, K, gH, R, offs, 0.0, of_group_d, K, R * K, _mode(mode))
+    handle.sgemm_grouped_depth(ec.OP_N, ec.OP_T, E, R, M, T, 1.0, H, R, gy, M, offs, 0.0, of_group_u, R, M * R, _mode(mode))
+    torch.cuda.synchronize()
+    gD, gU = torch.zeros_like(D), torch.zeros_like(U)
+    for e, a in enumerate(index):
+        if 0 <= a < A:
+            gD[a] += scales[a] * of_group_d[e]
+            gU[a] += scales[a] * of_group_u[e]
+    w, s = W.cpu().double(), scales.cpu().double()
+
+    def call(x, D, U):
+        out, at = [x[:start] @ w.t()], start
+        for n, a in zip(sizes, index):
+            rows = x[at:at + n]
+            out.append(rows @ w.t() + (s[a] * (rows @ D[a].t()) @ U[a].t() if 0 <= a < A else 0.0))
+            at += n
+        return torch.cat([*out, x[at:] @ w.t()])
+
+    leaves = [v.cpu().double().requires_grad_() for v in (x, D, U)]
+    want, g = call(*leaves), gy.cpu().double()
+    grads = torch.autograd.grad((want * g).sum(), leaves, allow_unused=True)
+    directions = torch.Generator().manual_seed(52)
+    for i, (got, ref) in enumerate(zip((gx, gD, gU), grads)):
+        ref, got = torch.zeros_like(leaves[i]) if ref is None else ref, got.cpu().double()
+        # two products after each other, as for the layer of experts; a sum of groups adds a rounding of its result for each of them
+        assert float((got - ref).norm()) <= (1.3e-5 + len(sizes) * 2.0 ** -24) * float(ref.norm())
+        # f is linear in each of its arguments: its difference is <gradient, d> but for the roundings of 64 bits
+        d = torch.randn(got.shape, generator=directions, dtype=torch.float64)
+        v = [l.detach() for l in leaves]
+        difference = float(((call(*[u + d if k == i else u for k, u in enumerate(v)]) - call(*v)) * g).sum())
+        rounding = 1e-9 * (1.0 + float(g.norm()) * float(want.detach().norm()))
+        assert abs(difference - float((ref * d).sum())) <= rounding
+        assert abs(difference - float((got * d).sum())) <= rounding + 1.4e-5 * float(ref.norm()) * float(d.norm())
+    assert float((y.cpu().double() - want.detach()).norm()) <= 1.3e-5 * float(want.detach().norm())
+    for a in range(A):
+        if a not in index:
+            assert not bool(gD[a].any()) and not bool(gU[a].any())
