@@ -350,9 +350,11 @@ ecgemm_status_t ecgemm_product(ecgemm_handle_t handle, int64_t M, int64_t N, int
  * beta == 0: C is not read.  K == 0 or alpha == 0: A and B are not read.  C must not overlap A or B.
  *
  * Groups of few columns (a decoding step), and groups of the depth that are shallow on average, are computed in FP32 on the
- * matrix unit, whichever mode is asked for: such a call is bound by reading A, or writing C, and its result is at least as
- * exact.  It follows from the sizes alone whether a call is.  An infinite or NaN value reaches the row of C or the columns
- * that it is multiplied into, and nothing else.
+ * matrix unit, whichever mode is asked for: such a call is bound by reading A, or writing C.  Values of any magnitude are
+ * multiplied as they are, and an element's products are added one after the other, each rounded to FP32, along the depth
+ * (groups of columns: in eight parts of it): more exact than the split for a short sum, and what a plain FP32 product is for a
+ * group that is much deeper than the mean.  It follows from sizes, storage orders and mode alone whether a call is.  An
+ * infinite or NaN value reaches the row of C or the columns that it is multiplied into, and nothing else.
  */
 #define ECGEMM_GROUPED_WORKSPACE_BYTES ((size_t)16 << 20)
 ecgemm_status_t ecgemm_sgemm_grouped(ecgemm_handle_t handle, ecgemm_op_t transA, ecgemm_op_t transB, int64_t groups,

@@ -3,8 +3,9 @@
 // Such a product reads its large operand once and does 2 n flop for every value of it, n columns: it is bound by memory
 // (n <= 32: at most 64 flop for 4 bytes, where the chip has 33 FP32 flop on the matrix unit for every byte that a copy
 // moves per second).  Splitting would add nothing, so the FP32 matrix instruction multiplies the values as they are:
-// v_mfma_f32_16x16x4_f32, 16 rows and 16 columns, four of the depth.  The result is at least as exact as either mode's,
-// values far from 1, infinities and NaN included.  What is arranged is the traffic:
+// v_mfma_f32_16x16x4_f32, 16 rows and 16 columns, four of the depth.  Values far from 1, infinities and NaN need no care.  An
+// element is off by at most 2^-24 of its products' magnitudes for each of the products that one wave adds up: an eighth of the
+// depth here, all of it in shallow_kernel.  What is arranged is the traffic:
 //   * a block takes 16 rows (64 where rows are contiguous) and all the group's columns, its eight waves share the depth
 //     between them, each taking every eighth stretch, so that the block reads runs of 1 KiB of every row; the eight sums
 //     meet in LDS and are added in order.

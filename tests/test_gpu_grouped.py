@@ -1016,3 +1016,53 @@ def test_gradients_of_adapters_that_requests_share(handle, mode, sizes, index):
     for a in range(A):
         if a not in index:
             assert not bool(gD[a].any()) and not bool(gU[a].any())
+
+
+@pytest.mark.parametrize("positive", [False, True])
+@pytest.mark.parametrize("trans", ["NT", "NN", "TT", "TN"])
+@pytest.mark.parametrize("M,N,groups,deep", [(70, 80, 300, 4800), (64, 200, 150, 9600), (257, 65, 64, 1000)])
+def test_one_group_as_deep_as_all_of_them(handle, trans, M, N, groups, deep, positive):
+    """Groups that are shallow on average, one of which has all the depth: its sums run along the depth in FP32.  Derived: a
+    fused multiply-add for each of n products, each rounded by 2^-24 of a sum that S bounds: n 2^-24 S, and 4 2^-24 S for
+    alpha and the rest.  And as close as the library promises of every product: the relative residual against 64 bits at most
+    1.25 times that of a naive FP32 product."""
+    import torch
+    from oracle import gemm
+    gen = _gen(61)
+    a_shape, b_shape = ((M, deep) if trans[0] == "N" else (deep, M)), ((deep, N) if trans[1] == "N" else (N, deep))
+    A, B = Field(*a_shape, gen=gen), Field(*b_shape, gen=gen)
+    if positive:
+        A.view().abs_(), B.view().abs_()
+    C = Field(M, N, count=groups, fill=7.0)
+    sizes = [0] * groups
+    sizes[groups // 3] = deep
+    for mode in MODES:
+        handle.sgemm_grouped_depth(_ops(trans[0]), _ops(trans[1]), groups, M, N, deep, 1.5, A.ptr(), A.ld, B.ptr(), B.ld, _offsets(sizes), 0.0,
+                                   C.ptr(), C.ld, C.stride, _mode(mode))
+        torch.cuda.synchronize()
+        a, b, got = A.matrix(trans[0]), B.matrix(trans[1]), C.view()[groups // 3].t()
+        exact = 1.5 * (a @ b)
+        assert bool(((got.double() - exact).abs() <= (deep + 4) * 2.0 ** -24 * 1.5 * (a.abs() @ b.abs())).all())
+        rows, cols = (np.asfortranarray(v.float().cpu().numpy()) for v in (a, b))
+        naive = gemm.sgemm_fp32_naive("N", "N", M, N, deep, 1.5, rows, cols)
+        assert gemm.relative_residual(exact.cpu().numpy(), got.cpu().numpy()) <= 1.25 * gemm.relative_residual(exact.cpu().numpy(), naive)
+        others = [g for g in range(groups) if g != groups // 3]
+        assert not bool(C.view()[others].any())
+
+
+def test_few_columns_of_a_great_depth(handle):
+    """The sums of few columns run along the depth in FP32, in eight parts."""
+    import torch
+    from oracle import gemm
+    gen, M, N, K = _gen(62), 4096, 5, 60000
+    A, B, C = Field(K, M, gen=gen), Field(K, N, gen=gen), Field(M, N, fill=7.0)
+    handle.sgemm_grouped(_ops("T"), _ops("N"), 1, M, N, K, 1.0, A.ptr(), A.ld, 0, B.ptr(), B.ld, _offsets([N]), 0.0, C.ptr(), C.ld, _mode("fp16"))
+    torch.cuda.synchronize()
+    a, b, got = A.matrix("T"), B.matrix("N"), C.view()[0].t()
+    exact = a @ b
+    # an eighth of the depth in a row, at most a stretch of 32 more, then eight sums one after the other
+    assert bool(((got.double() - exact).abs() <= (K / 8 + 32 + 8 + 4) * 2.0 ** -24 * (a.abs() @ b.abs())).all())
+    rows = 40
+    naive = gemm.sgemm_fp32_naive("N", "N", rows, N, K, 1.0, *(np.asfortranarray(v.float().cpu().numpy()) for v in (a[:rows], b)))
+    want = exact[:rows].cpu().numpy()
+    assert gemm.relative_residual(want, got[:rows].cpu().numpy()) <= 1.25 * gemm.relative_residual(want, naive)
