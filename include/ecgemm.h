@@ -333,19 +333,22 @@ ecgemm_status_t ecgemm_product(ecgemm_handle_t handle, int64_t M, int64_t N, int
  * operand, or decrease leave the results unspecified but nothing outside the operands is touched.
  *
  * Both modes of the method (ECGEMM_ERR_UNSUPPORTED for the others and for ECGEMM_MODE_AUTO), and the handle's pre-scaling
- * (ecgemm_set_scaling).  A forced kernel shape and the timing switch do not matter.  Leading dimensions of the operands up
- * to 2^21; M, N, K and the number of groups below 2^31.  Calls of few output tiles and a great depth cut the depth into
- * slices and put their sums into the handle's workspace, at most ECGEMM_GROUPED_WORKSPACE_BYTES of it; the others need none.
+ * (ecgemm_set_scaling).  A forced kernel shape and the timing switch do not matter, except to a projection with adapters that
+ * ecgemm_sgemm's kernels make.  Leading dimensions of the operands up to 2^21; M, N, K and the number of groups below 2^31.
+ * Calls of few output tiles and a great depth cut the depth into slices and put their sums into the handle's workspace, at
+ * most ECGEMM_GROUPED_WORKSPACE_BYTES of it; the others need none.
  * Each call runs on the handle's device whichever one is current.
  *
  * ecgemm_sgemm_grouped, groups of columns (a layer of experts; with transA the other way round its input's gradient):
  *     C(:, j) <- alpha * op(A_g) * op(B)(:, j) + beta * C(:, j)      for every column j of every group g
  *   A_g = A + g strideA; op(A_g) is M x K, op(B) is K x N, C is M x N, stored as for ecgemm_sgemm.  Columns in no group (before
- *   offsets[0], from offsets[groups] on) are left as they are, and so are those of op(B): never read.  strideA may be 0.
+ *   offsets[0], from offsets[groups] on) are left as they are, and what those of op(B) hold does not matter (with transB == T
+ *   a load may bring values of theirs, which are not used).  strideA may be 0.
  *
  * ecgemm_sgemm_grouped_depth, groups of the depth (the gradient of the experts' weights):
  *     C_g <- alpha * op(A)(:, k's of g) * op(B)(k's of g, :) + beta * C_g
- *   op(A) is M x K, op(B) is K x N, C_g = C + g strideC is M x N.  A group without any depth gives C_g <- beta * C_g.
+ *   op(A) is M x K, op(B) is K x N, C_g = C + g strideC is M x N, one behind the other: strideC >= ldc (N - 1) + M.  A group
+ *   without any depth gives C_g <- beta * C_g.
  *
  * beta == 0: C is not read.  K == 0 or alpha == 0: A and B are not read.  C must not overlap A or B.
  *
@@ -385,9 +388,10 @@ ecgemm_status_t ecgemm_sgemm_grouped_depth(ecgemm_handle_t handle, ecgemm_op_t t
  *      ecgemm_sgemm_grouped_depth with these groups gives the product of each group, without scales[a] (its alpha is one factor
  *      for all of them): the caller multiplies by it, adds up the groups that share an adapter, and drops those that have none.
  *      Where columns lie in the order of their adapters, one group for each adapter gives the sums themselves.
- * H times scales[a] / alpha is an operand like B: in FP16 mode it should lie in the window of the FP16 pair as well.  An adapter
- * that holds infinite or NaN values reaches its own columns only.
- * rank at most 1024; adapters below 2^31.  The projection uses the handle's workspace as ecgemm_sgemm does
+ * U and H times scales[a] / alpha are operands like A and B: in FP16 mode both should lie in the window of the FP16 pair, in either
+ * mode the latter in the range of FP32.  (Large calls split them; smaller ones multiply them in FP32 as they are, which goes by
+ * the sizes.)  An adapter that holds infinite or NaN values reaches its own columns only.
+ * rank at most 1024; adapters below 2^31; N below 2^27, M N below 2^38, K at most what ecgemm_sgemm takes.  The projection uses the handle's workspace as ecgemm_sgemm does
  * (ecgemm_workspace_size for M, N, K says how much).  C and H must not overlap each other or anything else.
  */
 ecgemm_status_t ecgemm_sgemm_adapters(ecgemm_handle_t handle, ecgemm_op_t transA, ecgemm_op_t transB, int64_t M, int64_t N,

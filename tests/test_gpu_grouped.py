@@ -1066,3 +1066,21 @@ def test_few_columns_of_a_great_depth(handle):
     naive = gemm.sgemm_fp32_naive("N", "N", rows, N, K, 1.0, *(np.asfortranarray(v.float().cpu().numpy()) for v in (a[:rows], b)))
     want = exact[:rows].cpu().numpy()
     assert gemm.relative_residual(want, got[:rows].cpu().numpy()) <= 1.25 * gemm.relative_residual(want, naive)
+
+
+def test_a_forced_shape_and_the_timing_switch_leave_groups_alone(handle):
+    """Equal bits with and without either; the projection of adapters may be made by ecgemm_sgemm's kernels, which follow both."""
+    import torch
+    ec = _ec()
+    want = [_run_columns(handle, "TN", "fp16", 300, 200, [100, 400]).store.clone(), _run_depth(handle, "NT", "bf16", 300, 200, [100, 400]).store.clone()]
+    other = ec.Handle()
+    other.set_stream(torch.cuda.current_stream().cuda_stream)
+    other.set_timing(True)
+    for shape in (ec.SHAPE_256x128_W4, ec.SHAPE_64x64_FUSED, ec.SHAPE_AUTO):
+        other.set_shape(shape)
+        got = [_run_columns(other, "TN", "fp16", 300, 200, [100, 400]).store, _run_depth(other, "NT", "bf16", 300, 200, [100, 400]).store]
+        assert all(torch.equal(g.nan_to_num(), w.nan_to_num()) for g, w in zip(got, want))
+        for mode in MODES:
+            _run_adapters(other, mode, 140, 200, 300, 16, [150, 40], [1, 0], 2, beta=0.5)
+    torch.cuda.synchronize()
+    other.destroy()
