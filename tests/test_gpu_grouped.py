@@ -1084,3 +1084,161 @@ def test_a_forced_shape_and_the_timing_switch_leave_groups_alone(handle):
             _run_adapters(other, mode, 140, 200, 300, 16, [150, 40], [1, 0], 2, beta=0.5)
     torch.cuda.synchronize()
     other.destroy()
+
+
+# more than 128 tiles: projection and adapters in one launch (A and U stored alike, the depth contiguous in B)
+_TILES = dict(M=2050, N=1100, K=150)
+
+
+@pytest.mark.parametrize("mode,rank", [("fp16", 20), ("fp16", 72), ("bf16", 20), ("bf16", 40)])
+@pytest.mark.parametrize("trans", ["TNTT", "NNNN", "TNNT", "NNTN"])
+def test_adapters_in_tiles(handle, trans, mode, rank):
+    """Adapters of a chunk and of more, several of them meeting in a tile, and columns without one."""
+    _run_adapters(handle, mode, **_TILES, rank=rank, sizes=[100, 1, 30, 0, 5, 400, 60, 17, 300], index=[2, 0, -1, 1, 3, 1, 7, 2, 0], adapters=4,
+                  trans=trans, start=3, alpha=1.5, beta=-0.5, pad=1)
+    _run_adapters(handle, mode, 2048, 1152, 128, rank, [128, 300, 724], [1, -1, 0], 2, trans=trans)
+
+
+@pytest.mark.parametrize("mode,rank", [("fp16", 20), ("fp16", 72), ("bf16", 20), ("bf16", 40)])
+@pytest.mark.parametrize("trans", ["TNTT", "NNNN", "TNNT", "NNTN"])
+def test_an_adapter_that_is_not_finite_in_tiles(handle, trans, mode, rank):
+    """Tiles that hold columns of such adapters, of sound ones and of none are made again for each of them: the others' bits are
+    those without it, and C, which is added to, is added once."""
+    import torch
+    ec, gen = _ec(), _gen(71)
+    M, N, K = (_TILES[k] for k in "MNK")
+    sizes, index, start = [200, 90, 7, 33, 300, 250, 150], [0, 1, -1, 3, 2, 0, 3], 5
+
+    def operand(rows, cols, t, **more):
+        return Field(rows, cols, gen=gen, **more) if t == "N" else Field(cols, rows, gen=gen, **more)
+
+    A, B = operand(M, K, trans[0]), operand(K, N, trans[1])
+    D, U = operand(rank, K, trans[2], count=4), operand(M, rank, trans[3], count=4)
+    scales = torch.tensor([0.5, 1.5, -2.0, 1.0], device="cuda")
+    results = []
+    for spoilt in (False, True):
+        if spoilt:
+            U.view()[1].fill_(float("nan"))
+            U.view()[2][rank - 1 if trans[3] == "N" else 1999, 1999 if trans[3] == "N" else rank - 1] = float("inf")
+            D.view()[3][3, 5] = float("inf")
+        H, C = Field(rank, N, fill=7.0), Field(M, N, values=torch.full((1, N, M), 0.25, device="cuda"), fill=7.0)
+        handle.sgemm_adapters(_ops(trans[0]), _ops(trans[1]), M, N, K, 1.0, A.ptr(), A.ld, B.ptr(), B.ld, len(sizes), _offsets(sizes, start),
+                              torch.tensor(index, dtype=torch.int32, device="cuda"), 4, rank, _ops(trans[2]), D.ptr(), D.ld, D.stride,
+                              _ops(trans[3]), U.ptr(), U.ld, U.stride, scales, H.ptr(), H.ld, 2.0, C.ptr(), C.ld, _mode(mode))
+        torch.cuda.synchronize()
+        results.append((C.view()[0].clone(), H.view()[0].clone()))
+        field = C.store.clone()
+        field.as_strided((N, M), (C.ld, 1), C.at).fill_(7.0)
+        assert bool((field == 7.0).all())
+    (clean, h_clean), (bad, h_bad) = results
+    of = torch.full((N,), -1)
+    at = start
+    for n, a in zip(sizes, index):
+        of[at:at + n] = a
+        at += n
+    of = of.cuda()
+    sound = (of == -1) | (of == 0)
+    assert bool(torch.isfinite(clean).all()) and torch.equal(clean[sound], bad[sound])
+    assert torch.equal(h_clean[of != 3], h_bad[of != 3])
+    assert bool(torch.isnan(bad[of == 1]).all())
+    others = torch.arange(M, device="cuda") != 1999        # of the one infinite value of U_2: its row alone
+    assert torch.equal(clean[of == 2][:, others], bad[of == 2][:, others]) and not bool(torch.isfinite(bad[of == 2][:, 1999]).any())
+    assert not bool(torch.isfinite(bad[of == 3]).any())
+
+
+@pytest.mark.parametrize("trans", ["TN", "TT"])
+def test_few_columns_in_blocks_of_two_rows(handle, trans):
+    """More than 16 columns to a group and 256 blocks of 32 rows: a block takes that many."""
+    rng = np.random.RandomState(81)
+    for K in (200, 33):
+        _run_columns(handle, trans, "fp16", 261, K, list(rng.randint(17, 32, 32)), start=1, behind=2, alpha=1.5, beta=-0.5, pad=(1, 2, 3), seed=K)
+    _run_columns(handle, trans, "bf16", 256, 192, [32, 1, 17, 63, 0, 33, 40, 16] * 4)
+
+
+@pytest.mark.parametrize("trans", ["TNTT", "TNNT", "NNNN", "NNTN"])
+@pytest.mark.parametrize("rank", [17, 20, 64, 100])
+def test_adapters_of_many_columns_in_blocks_of_two_rows(handle, trans, rank):
+    """H of more than 8160 columns in blocks of 32 of them, adapters meeting within a block."""
+    sizes, index = [3000, 1, 2, 29, 0, 1500, 40, 3600], [0, 2, 1, 0, 1, 2, -1, 1]
+    _run_adapters(handle, "fp16", 20, 8200, 90, rank, sizes, index, 3, trans=trans, start=7, pad=1, seed=rank)
+    _run_adapters(handle, "bf16", 5, 8192, 64, rank, [4096, 4096], [1, 0], 2, trans=trans, beta=0.5, seed=rank)
+
+
+@pytest.mark.parametrize("trans", ["TNTT", "TTTN"])
+def test_adapters_of_few_columns_in_blocks_of_two_rows(handle, trans):
+    """A projection of 8161 rows or more and 17 columns or more."""
+    rng = np.random.RandomState(82)
+    for M, N, K in ((8200, 40, 300), (8161, 17, 65), (8192, 64, 256)):
+        _run_adapters(handle, "fp16", M, N, K, 12, [1] * (N - 3) + [2], list(rng.randint(-1, 4, N - 2)), 4, trans=trans, beta=0.5, seed=N)
+
+
+@pytest.mark.parametrize("mode", MODES)
+def test_adapters_whose_projection_is_a_product_of_its_own(handle, mode):
+    """C of the adapters first, the projection added by ecgemm_sgemm's kernels: with a pre-scaling, an alpha by which H is not to
+    be divided, a great depth, A and U stored differently, and more requests than meet in a tile."""
+    import torch
+    for alpha, beta in ((2.0 ** -20, 0.0), (2.0 ** 18, 2.0 ** 18)):
+        _run_adapters(handle, mode, **_TILES, rank=20, sizes=[500, 1, 590], index=[1, -1, 0], adapters=2, start=3, alpha=alpha, beta=beta)
+    _run_adapters(handle, mode, M=2050, N=1100, K=6200, rank=20, sizes=[500, 1, 590], index=[1, -1, 0], adapters=2, beta=1.0, start=3, pad=1)
+    _run_adapters(handle, mode, **_TILES, rank=8, sizes=[500, 600], index=[1, 0], adapters=2, trans="NNNT", beta=1.0)
+    _run_adapters(handle, mode, **_TILES, rank=8, sizes=[9] * 122, index=[1, 0] * 61, adapters=2, start=1)
+    other = _ec().Handle()
+    other.set_stream(torch.cuda.current_stream().cuda_stream)
+    other.set_scaling(2, 3)
+    _run_adapters(other, mode, **_TILES, rank=8, sizes=[500, 600], index=[1, 0], adapters=2, beta=1.0)
+    torch.cuda.synchronize()
+    other.destroy()
+
+
+def test_captured_calls_that_use_the_workspace(handle):
+    """Slices of the depth and a projection that is split first, in a graph on a caller's workspace, between eager calls of another
+    handle: every replay has the bits of the eager call."""
+    import torch
+    ec, gen = _ec(), _gen(91)
+    T, K, M, R, N = 3000, 300, 200, 8, 1024
+    x, g = torch.randn((T, K), generator=gen, device="cuda"), torch.randn((T, M), generator=gen, device="cuda")
+    W, rows = torch.randn((2048, 7000), generator=gen, device="cuda") / 80, torch.randn((N, 7000), generator=gen, device="cuda")
+    D, U = torch.randn((2, R, 7000), generator=gen, device="cuda") / 80, torch.randn((2, 2048, R), generator=gen, device="cuda")
+    offs, offs_n, index = torch.zeros(3, dtype=torch.int64, device="cuda"), torch.zeros(3, dtype=torch.int64, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+
+    def calls(h, dw, y, hidden):
+        h.sgemm_grouped_depth(ec.OP_N, ec.OP_T, 2, K, M, T, 1.0, x, K, g, M, offs, 0.0, dw, K, M * K, ec.MODE_FP16_SPLIT)
+        h.sgemm_adapters(ec.OP_T, ec.OP_N, 2048, N, 7000, 1.0, W, 7000, rows, 7000, 2, offs_n, index, 2, R, ec.OP_T, D, 7000, R * 7000, ec.OP_T, U, R,
+                         2048 * R, None, hidden, R, 0.0, y, 2048, ec.MODE_BF16_FULL)
+
+    outs = [torch.zeros((2, M, K), device="cuda"), torch.zeros((N, 2048), device="cuda"), torch.zeros((N, R), device="cuda")]
+    captured, eager = ec.Handle(), ec.Handle()
+    eager.set_stream(torch.cuda.current_stream().cuda_stream)
+    nbytes = max(ec.GROUPED_WORKSPACE_BYTES, captured.workspace_size(ec.OP_T, ec.OP_N, 2048, N, 7000, ec.MODE_BF16_FULL))
+    workspace = torch.full((nbytes // 4 + 64,), 3.0, device="cuda")
+    captured.set_workspace(workspace, nbytes)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured.set_stream(torch.cuda.current_stream().cuda_stream)
+        calls(captured, *outs)
+    for sizes, ids in (([1000, 2000], [0, 1]), ([3000, 0], [1, 1]), ([1, 2], [-1, 0]), ([1500, 1500], [1, -1])):
+        offs.copy_(_offsets(sizes)), offs_n.copy_(_offsets([s // 3 for s in sizes])), index.copy_(torch.tensor(ids, dtype=torch.int32, device="cuda"))
+        want = [torch.full_like(o, 5.0) for o in outs]
+        calls(eager, *want)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for o, w in zip(outs, want):
+            assert torch.equal(o, w)
+    assert bool((workspace[nbytes // 4:] == 3.0).all())
+    captured.destroy(), eager.destroy()
+
+
+@pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("trans", ["TN", "NN", "TT", "NT"])
+def test_scaling_in_every_storage_order(handle, trans, mode):
+    """The handle's pre-scaling in tiles, whole and ragged, and in slices of the depth."""
+    handle.set_scaling(6, -3)
+    try:
+        _run_columns(handle, trans, mode, 300, 200, [150, 3, 400], start=1, behind=2, alpha=0.5, beta=2.0, pad=(1, 2, 3), scaling=(6, -3))
+        _run_columns(handle, trans, mode, 256, 192, [256, 384], scaling=(6, -3))
+        _run_depth(handle, trans, mode, 300, 200, [150, 0, 401], start=1, beta=1.0, pad=(1, 2, 3), scaling=(6, -3))
+        _run_depth(handle, trans, mode, 130, 90, [2000, 3, 4001], alpha=1.5, scaling=(6, -3))
+    finally:
+        handle.set_scaling(0, 0)
