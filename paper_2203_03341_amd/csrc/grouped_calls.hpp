@@ -36,7 +36,8 @@ int64_t most_grouped_tiles(bool along_depth, int64_t groups, int64_t M, int64_t 
 }
 
 // Slices of the depth: where the tiles are few, as many as fill the chip, 512 deep at least, and only if that saves more than
-// the 7 us that adding them up takes.  At most 256 tiles of partial sums: ECGEMM_GROUPED_WORKSPACE_BYTES.
+// the 7 us that adding them up takes, by the 0.95 us of a chunk of 64 in FP16 mode (1.5 in BF16 mode, which is cut by the same
+// rule).  At most 256 tiles of partial sums: ECGEMM_GROUPED_WORKSPACE_BYTES.
 int grouped_slices(int64_t tiles, int64_t depth) {
   const int64_t slices = std::min<int64_t>(kPlanComputeUnits / std::max<int64_t>(tiles, 1), std::min<int64_t>(depth / 512, 64));
   return slices >= 2 && depth / 64.0 * (1.0 - 1.0 / slices) * 0.95 > 8.0 ? (int)slices : 1;
@@ -89,6 +90,12 @@ ecgemm_status_t launch_grouped(ecgemm_handle_t h, ecgemm_mode_t mode, bool depth
 }
 
 // The kernels for few columns to a group (narrow_kernel.hpp).
+// H of adapters: by group below that many columns on average, else by columns of B.  Calls with M = 0, us, by group / by columns, B
+// with the depth contiguous, requests of 1, 4, 8, 16 and 32 columns: D with the depth contiguous, K 4096, rank 16, 32 requests
+// 10.2 / 65, 10.2 / 19, 10.2 / 11.7, 10.2 / 11.6, 14.1 / 12.3, K 2048, rank 64, 128 of them 11.1 / 99, 11.7 / 29, 14.3 / 18.6,
+// 19.3 / 19.7, 21.0 / 26.9; D with the rank contiguous, 4096, 16, 32 24 / 60, 24 / 18, 24 / 10.9, 24 / 11.0, 39 / 11.5, 2048, 64, 128
+// 15.9 / 91, 15.8 / 26.8, 15.8 / 17.6, 15.9 / 19.0, 24 / 28.  (B with the columns contiguous, D with the depth: 10 / 660, 9.9 / 177,
+// 9.9 / 93, 9.9 / 51, 14.5 / 31: the rule is made for the other order.)
 constexpr int64_t kAdapterDownMeanColumns = 8, kNarrowProjectionColumns = 64;
 constexpr int64_t kShallowMeanDepth = 16, kShallowMeanDepthSlim = 64;
 constexpr int64_t kAdapterOneLaunchDepth = 6144, kAdapterOneLaunchChunks = 8, kAdapterOneLaunchTiles = 128;
