@@ -1242,3 +1242,69 @@ def test_scaling_in_every_storage_order(handle, trans, mode):
         _run_depth(handle, trans, mode, 130, 90, [2000, 3, 4001], alpha=1.5, scaling=(6, -3))
     finally:
         handle.set_scaling(0, 0)
+
+
+def test_columns_in_tiles_of_several_launches(handle):
+    """More than 1024 groups, each with a matrix of its own, of more columns than the kernel of few columns takes."""
+    rng = np.random.RandomState(101)
+    _run_columns(handle, "TN", "fp16", 9, 10, list(rng.randint(60, 260, 1100)), start=2, behind=1, pad=(1, 0, 1))
+
+
+@pytest.mark.parametrize("trans", ["TN", "NN", "TT", "NT"])
+def test_the_largest_leading_dimensions(handle, trans):
+    """2^21 from one column to the next, in tiles, with few columns, and in shallow groups."""
+    def pads(*rows):
+        return tuple((1 << 21) - r for r in rows)
+
+    def stored(rows, cols, t):
+        return rows if t == "N" else cols
+
+    M, K = 130, 97
+    for mode in MODES:
+        N = 140
+        _run_columns(handle, trans, mode, M, K, [N], alpha=1.5, pad=(*pads(stored(M, K, trans[0]), stored(K, N, trans[1])), 1))
+    N = 19
+    _run_columns(handle, trans, "fp16", M, K, [N], pad=(*pads(stored(M, K, trans[0]), stored(K, N, trans[1])), 1))
+    M, N = 129, 130
+    for sizes in ([200], [5, 9]):
+        K = sum(sizes)
+        _run_depth(handle, trans, "fp16", M, N, sizes, pad=(*pads(stored(M, K, trans[0]), stored(K, N, trans[1])), 1))
+
+
+@pytest.mark.parametrize("N", [30, 400])
+def test_the_first_half_of_adapters_alone(handle, N):
+    """No rows of C: H all the same, and neither A nor U nor C is looked at."""
+    import torch
+    ec, gen, K, R = _ec(), _gen(111), 90, 12
+    x, D = torch.randn((N, K), generator=gen, device="cuda"), torch.randn((2, R, K), generator=gen, device="cuda")
+    H, sizes = torch.full((N, R), 7.0, device="cuda"), [N // 2, N // 4]
+    handle.sgemm_adapters(ec.OP_T, ec.OP_N, 0, N, K, 1.0, None, 0, x, K, 2, _offsets(sizes), torch.tensor([1, 0], dtype=torch.int32, device="cuda"),
+                          2, R, ec.OP_T, D, K, R * K, ec.OP_T, None, 0, 0, None, H, R, 0.0, None, 0, ec.MODE_FP16_SPLIT)
+    torch.cuda.synchronize()
+    at = 0
+    for n, a in zip(sizes, (1, 0)):
+        b, d = x[at:at + n].double(), D[a].double().t().contiguous()
+        assert bool(((H[at:at + n].double() - b @ d).abs() <= _allowed(b, d, "fp16", 1.0, 0.0, None)).all())
+        at += n
+    assert not bool(H[at:].any())
+
+
+@pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("M,N", [(2050, 1100), (300, 600), (300, 24)])
+def test_a_scale_that_is_not_finite_stays_with_its_adapter(handle, mode, M, N):
+    import torch
+    ec, gen, K, R = _ec(), _gen(112), 150, 12
+    W, x = torch.randn((M, K), generator=gen, device="cuda"), torch.randn((N, K), generator=gen, device="cuda")
+    D, U = torch.randn((3, R, K), generator=gen, device="cuda"), torch.randn((3, M, R), generator=gen, device="cuda")
+    sizes, index, results = [N // 4, N // 6, N // 6], [0, 1, 2], []
+    for scales in ([0.5, 1.0, 2.0], [0.5, float("nan"), float("inf")]):
+        y, H = torch.full((N, M), 0.25, device="cuda"), torch.full((N, R), 7.0, device="cuda")
+        handle.sgemm_adapters(ec.OP_T, ec.OP_N, M, N, K, 1.0, W, K, x, K, 3, _offsets(sizes), torch.tensor(index, dtype=torch.int32, device="cuda"),
+                              3, R, ec.OP_T, D, K, R * K, ec.OP_T, U, R, M * R, torch.tensor(scales, device="cuda"), H, R, 2.0, y, M, _mode(mode))
+        torch.cuda.synchronize()
+        results.append((y, H))
+    (clean, h_clean), (bad, h_bad) = results
+    at = np.cumsum([0, *sizes])
+    others = [*range(at[1]), *range(at[3], N)]
+    assert torch.equal(h_clean, h_bad) and torch.equal(clean[others], bad[others]) and bool(torch.isfinite(clean).all())
+    assert bool(torch.isnan(bad[at[1]:at[2]]).all()) and not bool(torch.isfinite(bad[at[2]:at[3]]).any())
