@@ -391,8 +391,9 @@ ecgemm_status_t ecgemm_sgemm_grouped_depth(ecgemm_handle_t handle, ecgemm_op_t t
  * U and H times scales[a] / alpha are operands like A and B: in FP16 mode both should lie in the window of the FP16 pair, in either
  * mode the latter in the range of FP32.  (Large calls split them; smaller ones multiply them in FP32 as they are, which goes by
  * the sizes.)  An adapter that holds infinite or NaN values reaches its own columns only.
- * rank at most 1024; adapters below 2^31; N below 2^27, M N below 2^38, K at most what ecgemm_sgemm takes.  The projection uses the handle's workspace as ecgemm_sgemm does
- * (ecgemm_workspace_size for M, N, K says how much).  C and H must not overlap each other or anything else.
+ * rank at most 1024; adapters below 2^31; N below 2^27, M N below 2^38, K at most what ecgemm_sgemm takes.  The projection uses
+ * the handle's workspace as ecgemm_sgemm does (ecgemm_workspace_size for M, N, K says how much).  C and H must not overlap each
+ * other or anything else.
  */
 ecgemm_status_t ecgemm_sgemm_adapters(ecgemm_handle_t handle, ecgemm_op_t transA, ecgemm_op_t transB, int64_t M, int64_t N,
                                       int64_t K, float alpha, const float *A, int64_t lda, const float *B, int64_t ldb,
